@@ -65,6 +65,8 @@ enum {
 #define MORE_K_MAX 32     /* largest k */
 #define MORE_R_MAX 1024   /* largest r (generic path); the tensor-core path takes r <= 64 */
 #define MORE_M_MAX (1 << 30) /* largest M: expert ids, and the kernels' column arithmetic, are 32-bit */
+#define MORE_H_MAX 8192   /* largest h of more_experts* and more_combine* */
+#define MORE_S_MAX 8192   /* largest width s of an expert */
 
 /*
  * more_route -- route T tokens (Algorithm 1 plus the gates of Section 2 / Eq. app_softmax and the per-expert
@@ -220,6 +222,111 @@ int more_merge_shards(const int32_t* idx, const float* topval, const float* lse,
  */
 int more_dispatch(const int32_t* idx, const int32_t* counts, int T, int k, int M,
                   int32_t* out_offsets, int32_t* out_sorted_pairs, void* stream);
+
+/*
+ * more_experts -- the experts' gated feed-forward blocks over the pairs of a routing (the layer's "expert linear 1, SwiGLU,
+ * expert linear 2"; M = 1, k = 1 with ids of 0 is the dense block):
+ *
+ *     u = X[t] W1[e],   a = silu(u_gate) * u_up,   Y[p] = a W2[e]         p = t*k + slot,  e = idx[p]
+ *
+ *   X          device bf16 [T][h];  W1 device bf16 [M][h][2s], an expert's s gate columns before its s others;  W2 device bf16
+ *              [M][s][h].  16-byte aligned; h and s multiples of 8, at most MORE_H_MAX and MORE_S_MAX.  Values must be finite.
+ *   idx        device int32 [T][k]: more_route's out_idx.
+ *   offsets, sorted_pairs   more_dispatch's outputs for the same ids.  Both may be NULL: then every pair reads its expert's weights
+ *              by itself, which is what few tokens do anyway -- a decoding step needs no dispatch.  With more pairs that is
+ *              slow, but right.  The results do not depend on the order of pairs inside an expert's run.
+ *   out_y      device bf16 [T*k][h], 16-byte aligned: the rows of a token's slots are next to one another (more_combine joins
+ *              them).  Rows of pairs whose id is outside [0, M) are not written.
+ *   out_hidden device bf16 [T*k][2s] or NULL: u of the pair in each place of sorted_pairs, which more_experts_backward reads.
+ *              Needs offsets and sorted_pairs.  Places past offsets[M] are not written.
+ *   path       MORE_EXPERTS_*; results differ in rounding only: tiles round the activation a to bf16 (it is an operand of the
+ *              second product), pairs do not.
+ *   workspace  device memory of at least more_experts_workspace(T, h, s, M, k, 0) bytes, 256-byte aligned, that nothing else uses
+ *              until the call's work is done (too little: MORE_ERR_TOO_LARGE).  The path with a CTA cluster per pair needs none.
+ * Products of bf16 are exact, sums are 32-bit.  Asynchronous on `stream`; the library's own scratch is not used, so calls with
+ * workspaces of their own may overlap, and calls may be captured into graphs (after a first call on the device).
+ */
+enum {
+    MORE_EXPERTS_AUTO = 0,
+    MORE_EXPERTS_PAIRS = 1,   /* a cluster of CTAs per pair; no out_hidden */
+    MORE_EXPERTS_TILES = 2    /* tcgen05 products of up to 128 pairs of an expert; needs offsets and sorted_pairs */
+};
+int more_experts(const void* X, const void* W1, const void* W2, const int32_t* idx, const int32_t* offsets,
+                 const int32_t* sorted_pairs, int T, int h, int s, int M, int k, void* out_y, void* out_hidden, int path,
+                 void* workspace, long long workspace_bytes, void* stream);
+
+/* more_experts_workspace -- bytes of workspace of more_experts (backward = 0) or more_experts_backward (1); or an error code. */
+long long more_experts_workspace(int T, int h, int s, int M, int k, int backward);
+
+/* more_experts_path -- which path MORE_EXPERTS_AUTO takes where dispatch lists are given and out_hidden is not; or an error code. */
+int more_experts_path(int T, int h, int s, int M, int k);
+
+/*
+ * more_experts_backward -- gradients of out[t] = sum_j gate[t][j] Y[t*k + j], Y = more_experts(X, ...), given the gradient at out:
+ *
+ *     c = dout[t] W2[e]^T,   dgate[p] = <c, a>,   du = gate c (silu'(u_gate) u_up, silu(u_gate))
+ *     dX[t] = sum_j du W1[e]^T,   dW1[e] = sum_p X[t]^T du,   dW2[e] = sum_p (gate a)^T dout[t]
+ *
+ *   X, W1, W2, idx, offsets, sorted_pairs   as in the forward call (the lists are required here).
+ *   gate       device fp32 [T][k];  hidden  the forward call's out_hidden for the same lists;  dout  device bf16 [T][h].
+ *   out_dx     device bf16 [T][h], out_dgate device fp32 [T][k], out_dw1 bf16 as W1, out_dw2 bf16 as W2; OVERWRITTEN (experts
+ *              without pairs get zeros; the gate gradient of a pair whose id is outside [0, M) is 0); any of them may be NULL.
+ *   workspace  as above, more_experts_workspace(T, h, s, M, k, 1) bytes.
+ * The Y rows are not needed: <dout, a W2> = <dout W2^T, a>.  The order of sums is that of sorted_pairs: equal lists give equal bits.
+ * Rounded to bf16 on the way: du and gate a, as operands of the products behind them; a slot's part of dX is kept in fp16 behind a
+ * power of two per row and 128 columns.
+ */
+int more_experts_backward(const void* X, const void* W1, const void* W2, const int32_t* idx, const int32_t* offsets,
+                          const int32_t* sorted_pairs, const float* gate, const void* hidden, const void* dout, int T, int h, int s,
+                          int M, int k, void* out_dx, float* out_dgate, void* out_dw1, void* out_dw2, void* workspace,
+                          long long workspace_bytes, void* stream);
+
+/*
+ * more_combine -- joins the rows of a token's slots to the residual stream, with a norm behind the block and one in front of the
+ * next (whose X it makes: the router's input):
+ *
+ *     y = sum_j gate[t][j] Y[t*k + j],   n = w_post * y / rms(y),   r' = residual + scale * n,   x = w_pre * r' / rms(r')
+ *     rms(v) = sqrt(mean(v^2) + eps)
+ *
+ *   Y          device bf16 [T*k][h], or NULL: nothing to join, r' = residual (the first block's norm).  A dense block's output is
+ *              k = 1.  A slot whose gate is 0 adds nothing and its row is not read.
+ *   gate       device fp32 [T][k], or NULL: ones.
+ *   residual   device [T][h] of residual_type, or NULL: zeros (not both Y and residual).
+ *   w_post, scale, w_pre   device fp32 [h], or NULL: no norm behind the block; no scale; no norm in front of the next.
+ *   out_residual  device [T][h] of residual_type or NULL; may be `residual` itself.
+ *   out_x      device bf16 [T][h] or NULL (needs w_pre);  out_sum  device bf16 [T][h] or NULL: y, which more_combine_backward
+ *              reads.  At least one output.
+ * h a multiple of 8, at most MORE_H_MAX; all pointers to rows and weights 16-byte aligned.  Everything between the inputs and the
+ * outputs is 32-bit: x is computed from the unrounded r'.  Asynchronous on `stream`; no workspace.
+ */
+enum { MORE_RESIDUAL_BF16 = 0, MORE_RESIDUAL_FP32 = 1 };   /* residual_type */
+int more_combine(const void* Y, const float* gate, const void* residual, int residual_type, const float* w_post, const float* scale,
+                 const float* w_pre, float eps, int T, int h, int k, void* out_residual, void* out_x, void* out_sum, void* stream);
+
+/*
+ * more_combine_backward -- gradients of more_combine at `residual` and at y, and of its weights, given those at r' and at x:
+ *
+ *     g = dresidual + (v - rh mean(rh v)) / rms(r'),  v = w_pre dx,  rh = r' / rms(r');      out_dresidual = g
+ *     out_dsum = (u - yh mean(yh u)) / rms(y),  u = scale w_post g,  yh = y / rms(y)
+ *     dscale = w_post sum_t g yh,   dw_post = scale sum_t g yh,   dw_pre = sum_t dx rh
+ *
+ *   dresidual  device [T][h] of residual_type, or NULL: zeros;  dx  device bf16 [T][h], or NULL: zeros (not both).
+ *   sum        out_sum of the forward call (may be NULL where no norm stood behind the block and neither out_dscale nor
+ *              out_dw_post is asked for);  residual_out  its out_residual, required with dx.
+ *   w_post, scale, w_pre, eps   as in the forward call; w_pre is required with dx.
+ *   out_dresidual  device [T][h] of residual_type (may be `dresidual` itself), out_dsum device bf16 [T][h] (the dout of
+ *              more_experts_backward), out_dw_post, out_dscale, out_dw_pre device fp32 [h], OVERWRITTEN; any may be NULL, and must be
+ *              where the forward call had no such weight (out_dw_pre: where dx is NULL).
+ *   workspace  device, 16-byte aligned, more_combine_workspace(T, h) bytes; needed for the gradients of weights only.
+ * Sums over tokens are 32-bit, in an order that depends on T and h alone.  Asynchronous on `stream`.
+ */
+int more_combine_backward(const void* dresidual, const void* dx, const void* sum, const void* residual_out, int residual_type,
+                          const float* w_post, const float* scale, const float* w_pre, float eps, int T, int h, void* out_dresidual,
+                          void* out_dsum, float* out_dw_post, float* out_dscale, float* out_dw_pre, void* workspace,
+                          long long workspace_bytes, void* stream);
+
+/* more_combine_workspace -- bytes of workspace of more_combine_backward; or an error code. */
+long long more_combine_workspace(int T, int h);
 
 /*
  * more_route_plan -- report, without launching, what more_route_ex would do for a shape:

@@ -16,6 +16,7 @@ from . import build as _build
 GATE_TOPK_SOFTMAX = 0
 GATE_FULL_SOFTMAX = 1
 PATH_AUTO, PATH_GENERIC, PATH_TCGEN05 = 0, 1, 2
+EXPERTS_AUTO, EXPERTS_PAIRS, EXPERTS_TILES = 0, 1, 2
 K_MAX = 32
 
 _lib = None
@@ -57,6 +58,21 @@ def lib() -> ctypes.CDLL:
         L.more_route_noalloc.restype = i32
         L.more_route_noalloc_capacity.argtypes = []
         L.more_route_noalloc_capacity.restype = ctypes.c_longlong
+        i64, f32 = ctypes.c_longlong, ctypes.c_float
+        L.more_experts.argtypes = [vp] * 6 + [i32] * 5 + [vp, vp, i32, vp, i64, vp]
+        L.more_experts.restype = i32
+        L.more_experts_workspace.argtypes = [i32] * 6
+        L.more_experts_workspace.restype = i64
+        L.more_experts_path.argtypes = [i32] * 5
+        L.more_experts_path.restype = i32
+        L.more_experts_backward.argtypes = [vp] * 9 + [i32] * 5 + [vp] * 5 + [i64, vp]
+        L.more_experts_backward.restype = i32
+        L.more_combine.argtypes = [vp, vp, vp, i32, vp, vp, vp, f32, i32, i32, i32, vp, vp, vp, vp]
+        L.more_combine.restype = i32
+        L.more_combine_backward.argtypes = [vp] * 4 + [i32, vp, vp, vp, f32, i32, i32] + [vp] * 6 + [i64, vp]
+        L.more_combine_backward.restype = i32
+        L.more_combine_workspace.argtypes = [i32, i32]
+        L.more_combine_workspace.restype = i64
         ip = ctypes.POINTER(ctypes.c_int)
         L.more_route_plan.argtypes = [i32, i32, i32, i32, i32, i32, i32, i32, ip, ip, ip]
         L.more_route_plan.restype = i32
@@ -108,7 +124,9 @@ def _fast():
         module = importlib.util.module_from_spec(importlib.util.spec_from_loader("_more_binding", loader))
         loader.exec_module(module)
         module.bind(*[ctypes.cast(f, ctypes.c_void_p).value for f in
-                      (L.more_route_ex, L.more_route_psum, L.more_dispatch, L.more_route_full, L.more_merge_shards)])
+                      (L.more_route_ex, L.more_route_psum, L.more_dispatch, L.more_route_full, L.more_merge_shards, L.more_experts,
+                       L.more_experts_workspace, L.more_experts_path, L.more_experts_backward, L.more_combine,
+                       L.more_combine_backward, L.more_combine_workspace)])
         _fast_module = module
     return _fast_module
 
@@ -246,6 +264,69 @@ def more_merge_shards(idx, topval, lse, shard_base, M, gate_mode, out_idx, out_g
         raise MoreRouteError(rc, "more_merge_shards")
 
 
+def more_experts(X, W1, W2, idx, offsets, pairs, out_y, out_hidden=None, path=EXPERTS_AUTO, workspace=None, stream=None):
+    """``more_experts`` of the C interface: ``out_y [T*k,h]`` = the gated feed-forward blocks of the experts (``W1 [M,h,2s]``,
+    ``W2 [M,s,h]``, bf16) on the pairs of ``idx [T,k]``, given :func:`more_dispatch`'s ``offsets`` and ``pairs`` (both None for a
+    few tokens); ``out_hidden [T*k,2s]`` keeps what the backward pass reads.  ``workspace`` (uint8, at least
+    :func:`experts_workspace` bytes) is torch's memory of the call's stream where it is None."""
+    rc = (_fast_module or _fast()).experts(X, W1, W2, idx, offsets, pairs, out_y, out_hidden, False, path, workspace, stream)[0]
+    if rc != 0:
+        raise MoreRouteError(rc, "more_experts")
+
+
+def experts_workspace(T, h, s, M, k, backward=False) -> int:
+    """Bytes of workspace that :func:`more_experts` or :func:`more_experts_backward` needs for these sizes."""
+    n = int(lib().more_experts_workspace(T, h, s, M, k, int(backward)))
+    if n < 0:
+        raise MoreRouteError(n, "more_experts_workspace")
+    return n
+
+
+def experts_path(T, h, s, M, k) -> int:
+    """The path that :func:`more_experts` takes by itself where it has dispatch lists and no ``out_hidden``."""
+    n = int(lib().more_experts_path(T, h, s, M, k))
+    if n < 0:
+        raise MoreRouteError(n, "more_experts_path")
+    return n
+
+
+def more_experts_backward(X, W1, W2, idx, offsets, pairs, gate, hidden, dout, out_dx=None, out_dgate=None, out_dw1=None, out_dw2=None,
+                          workspace=None, stream=None):
+    """``more_experts_backward`` of the C interface: gradients at ``X``, ``gate [T,k]``, ``W1`` and ``W2`` (those that are not None)
+    of ``sum_j gate[t,j] Y[t*k+j]``, given ``dout [T,h]`` and the forward call's ``out_hidden`` for the same lists."""
+    rc = (_fast_module or _fast()).experts_backward(X, W1, W2, idx, offsets, pairs, gate, hidden, dout, out_dx, out_dgate, out_dw1,
+                                                    out_dw2, 0, workspace, stream)[0]
+    if rc != 0:
+        raise MoreRouteError(rc, "more_experts_backward")
+
+
+def more_combine(Y, gate, residual, w_post, scale, w_pre, eps, out_residual=None, out_x=None, out_sum=None, k=0, stream=None):
+    """``more_combine`` of the C interface: ``Y [T*k,h]`` joined by ``gate [T,k]``, normed (``w_post``), scaled (``scale``) and added
+    to ``residual`` (bf16 or fp32 ``[T,h]``); ``out_x`` is the sum normed again (``w_pre``).  Everything but the outputs that
+    are wanted may be None; ``k`` is for rows without gates, residual and k = 1."""
+    rc = (_fast_module or _fast()).combine(Y, gate, residual, w_post, scale, w_pre, eps, k, out_residual, out_x, out_sum, 0, stream)[0]
+    if rc != 0:
+        raise MoreRouteError(rc, "more_combine")
+
+
+def more_combine_backward(dresidual, dx, sum, residual_out, w_post, scale, w_pre, eps, out_dresidual=None, out_dsum=None,
+                          out_dw_post=None, out_dscale=None, out_dw_pre=None, workspace=None, stream=None):
+    """``more_combine_backward`` of the C interface: gradients at the residual, at the joined rows (``out_dsum``, the ``dout`` of
+    :func:`more_experts_backward`) and of the three weights, those that are not None."""
+    rc = (_fast_module or _fast()).combine_backward(dresidual, dx, sum, residual_out, w_post, scale, w_pre, eps, out_dresidual, out_dsum,
+                                                    out_dw_post, out_dscale, out_dw_pre, 0, workspace, stream)[0]
+    if rc != 0:
+        raise MoreRouteError(rc, "more_combine_backward")
+
+
+def combine_workspace(T, h) -> int:
+    """Bytes of workspace that :func:`more_combine_backward` needs for these sizes."""
+    n = int(lib().more_combine_workspace(T, h))
+    if n < 0:
+        raise MoreRouteError(n, "more_combine_workspace")
+    return n
+
+
 def more_route_status(stream=None) -> int:
     return int(lib().more_route_status(_stream(stream)))
 
@@ -315,3 +396,73 @@ def route(X, R1, R2, k, gate_mode=GATE_TOPK_SOFTMAX, want_topval=False, want_lse
     if rc != 0:
         raise MoreRouteError(rc, "more_route_ex")
     return RouteResult(idx, gate, counts, topval, lse)
+
+
+@dataclass
+class ExpertsResult:
+    y: "object"
+    hidden: "object" = None
+
+
+def experts(X, W1, W2, idx, offsets=None, pairs=None, want_hidden=False, path=EXPERTS_AUTO, workspace=None, stream=None) -> ExpertsResult:
+    """Convenience wrapper: allocate the outputs with torch and do what :func:`more_experts` does.  Rows of pairs without an expert
+    are uninitialised."""
+    rc, y, hidden = (_fast_module or _fast()).experts(X, W1, W2, idx, offsets, pairs, None, None, want_hidden, path, workspace, stream)
+    if rc != 0:
+        raise MoreRouteError(rc, "more_experts")
+    return ExpertsResult(y, hidden)
+
+
+@dataclass
+class ExpertsGradients:
+    dx: "object"
+    dgate: "object"
+    dw1: "object"
+    dw2: "object"
+
+
+def experts_backward(X, W1, W2, idx, offsets, pairs, gate, hidden, dout, want_dx=True, want_dgate=True, want_dw=True, workspace=None,
+                     stream=None) -> ExpertsGradients:
+    """Convenience wrapper: allocate the gradients that are wanted and do what :func:`more_experts_backward` does."""
+    make = int(want_dx) + 2 * int(want_dgate) + 12 * int(want_dw)
+    rc, *grads = (_fast_module or _fast()).experts_backward(X, W1, W2, idx, offsets, pairs, gate, hidden, dout, None, None, None, None,
+                                                            make, workspace, stream)
+    if rc != 0:
+        raise MoreRouteError(rc, "more_experts_backward")
+    return ExpertsGradients(*grads)
+
+
+@dataclass
+class CombineResult:
+    residual: "object"
+    x: "object" = None
+    sum: "object" = None
+
+
+def combine(Y, gate, residual, w_post=None, scale=None, w_pre=None, eps=1e-6, k=0, want_sum=False, stream=None) -> CombineResult:
+    """Convenience wrapper: allocate the outputs (``x`` where there is ``w_pre``) and do what :func:`more_combine` does."""
+    make = 1 + 2 * int(w_pre is not None) + 4 * int(want_sum)
+    rc, *out = (_fast_module or _fast()).combine(Y, gate, residual, w_post, scale, w_pre, eps, k, None, None, None, make, stream)
+    if rc != 0:
+        raise MoreRouteError(rc, "more_combine")
+    return CombineResult(*out)
+
+
+@dataclass
+class CombineGradients:
+    dresidual: "object"
+    dsum: "object"
+    dw_post: "object"
+    dscale: "object"
+    dw_pre: "object"
+
+
+def combine_backward(dresidual, dx, sum, residual_out, w_post=None, scale=None, w_pre=None, eps=1e-6, workspace=None,
+                     stream=None) -> CombineGradients:
+    """Convenience wrapper: allocate the gradients (of the weights that are there) and do what :func:`more_combine_backward` does."""
+    make = 3 + 4 * int(w_post is not None) + 8 * int(scale is not None) + 16 * int(w_pre is not None and dx is not None)
+    rc, *grads = (_fast_module or _fast()).combine_backward(dresidual, dx, sum, residual_out, w_post, scale, w_pre, eps, None, None, None,
+                                                            None, None, make, workspace, stream)
+    if rc != 0:
+        raise MoreRouteError(rc, "more_combine_backward")
+    return CombineGradients(*grads)

@@ -1,0 +1,187 @@
+// The experts' feed-forward blocks for few (token, slot) pairs: decoding, where nearly every pair has an expert of its own and a
+// call is the time to read the weights of the experts that are hit.  No list of pairs, no workspace, one launch.
+//
+// A cluster of CTAs serves a pair.  Each takes a slice of the hidden dimension, in both products: its rows of W1 (one contiguous
+// piece of memory) give a part of every activation's sum, which the CTAs exchange through distributed shared memory (2 s floats
+// each); then its columns of W2 give its columns of the output, without a second exchange.  The first rows of W2 are requested
+// before the exchange, so that a call waits for memory about once.  Sums and the activation stay in 32 bits.
+#include "more_experts.cuh"
+
+namespace more {
+
+namespace {
+
+constexpr int kPThreads = 256;
+constexpr int kBatch = 8;                         // 16-byte loads in flight per thread
+
+__device__ __forceinline__ float ld_cluster(uint32_t addr, int rank)
+{
+    uint32_t remote;
+    float v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(addr), "r"(rank));
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(remote) : "memory");
+    return v;
+}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+
+__device__ __forceinline__ void fma8(float (&acc)[8], float x, const uint4& w)
+{
+    acc[0] = fmaf(x, bf16_lo(w.x), acc[0]); acc[1] = fmaf(x, bf16_hi(w.x), acc[1]);
+    acc[2] = fmaf(x, bf16_lo(w.y), acc[2]); acc[3] = fmaf(x, bf16_hi(w.y), acc[3]);
+    acc[4] = fmaf(x, bf16_lo(w.z), acc[4]); acc[5] = fmaf(x, bf16_hi(w.z), acc[5]);
+    acc[6] = fmaf(x, bf16_lo(w.w), acc[6]); acc[7] = fmaf(x, bf16_hi(w.w), acc[7]);
+}
+__device__ __forceinline__ uint4 ld_stream(const __nv_bfloat16* p)      // weights: read once
+{
+    uint4 v;
+    asm volatile("ld.global.nc.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
+}
+
+// Threads as `groups` column groups of 8 times as many row groups as fit: acc = sum over this thread's rows of x[row] W[row][8 columns].
+struct Slice {
+    const __nv_bfloat16* at;      // of this thread's first row, or nullptr
+    size_t step;                  // elements between its rows
+    int rows, row, stride;        // rows of the slice, its first, distance
+    __device__ void load(uint4 (&w)[kBatch], int from) const
+    {
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i)
+            w[i] = at && row + (from + i) * stride < rows ? ld_stream(at + (size_t)(from + i) * step) : make_uint4(0, 0, 0, 0);
+    }
+    __device__ void add(float (&acc)[8], const uint4 (&w)[kBatch], const float* x, int from) const
+    {
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+            const int r = row + (from + i) * stride;
+            if (at && r < rows) fma8(acc, x[r], w[i]);
+        }
+    }
+    __device__ void sum(float (&acc)[8], uint4 (&w)[kBatch], const float* x) const      // w: the first batch, loaded
+    {
+        const int mine = at && row < rows ? (rows - row + stride - 1) / stride : 0;
+        for (int i = 0; i < mine; i += kBatch) {
+            uint4 next[kBatch];
+            if (i + kBatch < mine) load(next, i + kBatch);
+            add(acc, w, x, i);
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j) w[j] = next[j];
+        }
+    }
+};
+
+// red[row group][8 columns of a group] -> the sum of column c of `cols`
+__device__ __forceinline__ float column_sum(const float* red, int cols, int row_groups, int c)
+{
+    float v = 0.f;
+    for (int r = 0; r < row_groups; ++r) v += red[r * cols + c];
+    return v;
+}
+
+__global__ void __launch_bounds__(kPThreads)
+pairs_kernel(const __nv_bfloat16* __restrict__ X, const __nv_bfloat16* __restrict__ W1, const __nv_bfloat16* __restrict__ W2,
+             const int32_t* __restrict__ idx, int h, int s, int M, int k, int ranks, __nv_bfloat16* __restrict__ Y)
+{
+    extern __shared__ float sm[];
+    float* red = sm;                                   // [256 x 8]
+    float* part = red + kPThreads * 8;                 // [2 s]
+    float* act = part + 2 * s;                         // [s]
+    float* x = act + s;                                // [slice]
+    const int tid = threadIdx.x, pair = blockIdx.x / ranks, rank = blockIdx.x % ranks;
+    const int e = idx[pair];
+    if ((unsigned)e >= (unsigned)M) return;            // no expert: the row stays as it is (all CTAs of the cluster agree)
+    const int per = (h / 8 + ranks - 1) / ranks, v0 = min(rank * per, h / 8), vn = min(per, h / 8 - v0);   // 16-byte vectors of the slice
+    const int rows = vn * 8;
+
+    // first product: columns in passes of up to 256 groups of 8
+    const __nv_bfloat16* w1 = W1 + ((size_t)e * h + v0 * 8) * 2 * s;
+    const int all = s / 4;
+    uint4 w[kBatch];
+    for (int g0 = 0; g0 < all; g0 += kPThreads) {
+        const int groups = min(all - g0, kPThreads), rg = kPThreads / groups;
+        const int mine = tid / groups, col = (g0 + tid % groups) * 8;
+        Slice sl{mine < rg ? w1 + (size_t)mine * 2 * s + col : nullptr, (size_t)rg * 2 * s, rows, mine, rg};
+        sl.load(w, 0);
+        if (g0 == 0) {
+            const __nv_bfloat16* from = X + (size_t)(pair / k) * h + v0 * 8;
+            for (int i = tid; i < rows; i += kPThreads) x[i] = __bfloat162float(from[i]);
+            __syncthreads();
+        }
+        float acc[8] = {};
+        sl.sum(acc, w, x);
+        if (mine < rg)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) red[mine * groups * 8 + (tid % groups) * 8 + i] = acc[i];
+        __syncthreads();
+        for (int c = tid; c < groups * 8; c += kPThreads) part[g0 * 8 + c] = column_sum(red, groups * 8, rg, c);
+        __syncthreads();
+    }
+    cluster_arrive();
+    // second product, first rows
+    const int passes = (vn + kPThreads - 1) / kPThreads;
+    auto slice2 = [&](int g0) {
+        const int groups = min(vn - g0, kPThreads), rg = groups > 0 ? kPThreads / groups : 0;
+        const int mine = groups > 0 ? tid / groups : 0;
+        return Slice{mine < rg ? W2 + ((size_t)e * s + mine) * h + (size_t)(v0 + g0 + tid % groups) * 8 : nullptr, (size_t)rg * h, s, mine, rg};
+    };
+    if (passes > 0) slice2(0).load(w, 0);
+    cluster_wait();
+    const uint32_t part_at = smem_u32(part);
+    for (int c = tid; c < s; c += kPThreads) {
+        float g = 0.f, u = 0.f;
+        for (int q = 0; q < ranks; ++q) {
+            g += ld_cluster(part_at + c * 4, q);
+            u += ld_cluster(part_at + (s + c) * 4, q);
+        }
+        act[c] = g * sigmoidf(g) * u;
+    }
+    __syncthreads();
+    cluster_arrive();                                  // (done with the other CTAs' parts)
+    for (int p = 0; p < passes; ++p) {
+        const int g0 = p * kPThreads, groups = min(vn - g0, kPThreads), rg = kPThreads / groups;
+        const Slice sl = slice2(g0);
+        if (p > 0) sl.load(w, 0);
+        float acc[8] = {};
+        sl.sum(acc, w, act);
+        if (tid / groups < rg)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) red[(tid / groups) * groups * 8 + (tid % groups) * 8 + i] = acc[i];
+        __syncthreads();
+        for (int c = tid * 2; c < groups * 8; c += kPThreads * 2) {
+            const float lo = column_sum(red, groups * 8, rg, c), hi = column_sum(red, groups * 8, rg, c + 1);
+            *reinterpret_cast<uint32_t*>(Y + (size_t)pair * h + (size_t)(v0 + g0) * 8 + c) = pack_bf16(lo, hi);
+        }
+        __syncthreads();
+    }
+    cluster_wait();
+}
+
+}  // namespace
+
+int launch_experts_pairs(const ExpertsArgs& a, const DeviceCtx& ctx)
+{
+    const long long P = (long long)a.T * a.k;
+    // CTAs per pair: as many as fill the SMs, but not less than 8 rows each
+    int ranks = 1;
+    while (ranks < 8 && P * ranks < 2LL * ctx.sm_count && a.h / (ranks * 2) >= 32) ranks *= 2;
+    const size_t smem = sizeof(float) * (kPThreads * 8 + 3 * (size_t)a.s + ((size_t)a.h / 8 + ranks - 1) / ranks * 8);
+    if (cudaFuncSetAttribute(pairs_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return MORE_ERR_CUDA;
+    if (P * ranks > 0x7fffffffLL) return MORE_ERR_TOO_LARGE;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)(P * ranks));
+    cfg.blockDim = dim3(kPThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = a.stream;
+    cudaLaunchAttribute at;
+    at.id = cudaLaunchAttributeClusterDimension;
+    at.val.clusterDim.x = (unsigned)ranks;
+    at.val.clusterDim.y = at.val.clusterDim.z = 1;
+    cfg.attrs = &at;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, pairs_kernel, a.X, a.W1, a.W2, a.idx, a.h, a.s, a.M, a.k, ranks, a.out_y) != cudaSuccess) return MORE_ERR_CUDA;
+    count_launch(1);
+    return cudaGetLastError() == cudaSuccess ? MORE_OK : MORE_ERR_CUDA;
+}
+
+}  // namespace more

@@ -115,4 +115,7 @@ int launch_dispatch(const int32_t* idx, const int32_t* counts, int T, int k, int
 
 void count_launch(int n = 1);
 
+// The state of the current device (an error code on another architecture); takes the library's lock itself.
+int device_ctx(DeviceCtx** out);
+
 }  // namespace more

@@ -185,6 +185,12 @@ int route_device(const RouteArgs& a, int path, int msplit)
 
 }  // namespace
 
+int device_ctx(DeviceCtx** out)
+{
+    std::lock_guard<std::mutex> lock(g_mutex);
+    return get_ctx(out);
+}
+
 void count_launch(int n) { g_launches.fetch_add(n, std::memory_order_relaxed); }
 
 namespace {

@@ -30,6 +30,8 @@
 //
 // Every mbarrier wait is bounded: when the budget runs out the thread records MORE_ERR_TIMEOUT in the device
 // status word, raises the CTA's abort flag and all roles fall through to the common exit (TMEM is freed there).
+#include <atomic>
+
 #include "sm100_common.cuh"
 #include "more_select.cuh"
 
@@ -886,13 +888,14 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t,
 
 EncodeTiledFn encode_fn()
 {
-    static EncodeTiledFn fn = nullptr;
+    static std::atomic<EncodeTiledFn> found{nullptr};
+    EncodeTiledFn fn = found.load(std::memory_order_relaxed);
     if (!fn) {
         void* sym = nullptr;
         cudaDriverEntryPointQueryResult qres;
         if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &sym, cudaEnableDefault, &qres) == cudaSuccess &&
             qres == cudaDriverEntryPointSuccess)
-            fn = reinterpret_cast<EncodeTiledFn>(sym);
+            found.store(fn = reinterpret_cast<EncodeTiledFn>(sym), std::memory_order_relaxed);
     }
     return fn;
 }
@@ -934,6 +937,23 @@ int get_tensor_map(const void* ptr, int rows, int cols, int box_rows, int box_co
     g_maps[slot] = m;
     *out = m;
     return MORE_OK;
+}
+
+int encode_tensor_map(const void* ptr, int rank, const uint64_t* dims, const uint64_t* strides, const uint32_t* box, CUtensorMap* out)
+{
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return MORE_ERR_CUDA;
+    cuuint64_t d[5], st[5];
+    cuuint32_t b[5], estr[5];
+    for (int i = 0; i < rank; ++i) {
+        d[i] = dims[i];
+        b[i] = box[i];
+        estr[i] = 1;
+        if (i + 1 < rank) st[i] = strides[i];
+    }
+    return fn(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank, const_cast<void*>(ptr), d, st, b, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
+               ? MORE_OK : MORE_ERR_CUDA;
 }
 
 namespace {

@@ -367,4 +367,7 @@ __device__ __forceinline__ void tc_mma_buffer_ss(uint32_t d, uint32_t a_lo, uint
 // fill out of bounds.  Descriptors are cached (host side, guarded by the API mutex).
 int get_tensor_map(const void* ptr, int rows, int cols, int box_rows, int box_cols, CUtensorMap* out);
 
+// The same for a bf16 tensor of `rank` dimensions, innermost first (strides in bytes, of all but the innermost), not cached.
+int encode_tensor_map(const void* ptr, int rank, const uint64_t* dims, const uint64_t* strides, const uint32_t* box, CUtensorMap* out);
+
 }  // namespace more
