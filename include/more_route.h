@@ -274,7 +274,7 @@ int more_experts_path(int T, int h, int s, int M, int k);
  *   workspace  as above, more_experts_workspace(T, h, s, M, k, 1) bytes.
  * The Y rows are not needed: <dout, a W2> = <dout W2^T, a>.  The order of sums is that of sorted_pairs: equal lists give equal bits.
  * Rounded to bf16 on the way: du and gate a, as operands of the products behind them; a slot's part of dX is kept in fp16 behind a
- * power of two per row and 128 columns.
+ * power of two per row and 32 columns.
  */
 int more_experts_backward(const void* X, const void* W1, const void* W2, const int32_t* idx, const int32_t* offsets,
                           const int32_t* sorted_pairs, const float* gate, const void* hidden, const void* dout, int T, int h, int s,

@@ -5,58 +5,50 @@
 //   c = d[token] W2[e]^T,  dgate = <c, a>,  du = gate c (silu'(u_gate) u_up, silu(u_gate)),  dX = sum over slots of du W1[e]^T
 //   dW1[e] = sum of X[token]^T du,  dW2[e] = sum of (gate a)^T d[token]
 //
-// Two kernels do all of it, both persistent with one CTA per SM: a TMA warp, a warp that issues the tcgen05 MMAs, eight warps
+// Two kernels do all of it, both persistent with one CTA per SM: warps that load, a warp that issues the tcgen05 MMAs, eight warps
 // that read the finished accumulator (two of 256 tensor-memory columns, used in turn, so that the products of the next unit run
 // meanwhile).
 //
-//   rows_kernel<MODE>   tiles of up to 128 pairs of one expert against its weights.  The rows of a tile are anywhere in X: they
-//                       come by gathering TMA loads (four rows of 128 bytes each), only as many as the tile has, and land in the
-//                       swizzled layout that the MMAs read.  W1 and W2 are used as they are stored, the forward products with
-//                       them as MN-major operands, the backward ones as K-major ones: nothing is transposed.
+//   rows_kernel<MODE>   tiles of up to 128 pairs of one expert against its weights.  W1 and W2 come by TMA and are used as they are
+//                       stored, the forward products with them as MN-major operands, the backward ones as K-major ones: nothing
+//                       is transposed.
 //   weights_kernel      dW of one expert: 128 x 256 outputs, contracted over the expert's pairs 64 at a time, both operands
-//                       MN-major from gathered rows; rows behind the last pair are out of the tensor's bounds and read as zeros.
+//                       MN-major.
+//
+// Rows that are anywhere in X or d come by gathering TMA loads, four rows of 128 bytes each, in the swizzled layout that the MMAs read;
+// four warps share them, as each costs its warp about 100 clocks.  (Asynchronous 16-byte copies by threads were slower: 144 us
+// against 105 for the first product of 16384 x 8 pairs, h = 512, 4096 experts of s = 64.)
 //
 // What bounds them: with the paper's narrow experts, the bytes: each expert's weights are read once (six bytes per h s) for as
-// few as 30 tokens.  So the loads of the next tiles are requested while a tile is computed, and what does not have to be kept
-// is not written: the activation goes to the second product as bf16 rows in expert order (s of them against h of an output row).
+// few as 30 tokens.  A stage of the ring in shared memory is as long as what it holds, so that tiles of few rows have more
+// weights in flight, and gradients of weights leave shared memory by TMA stores that nobody waits for.  The activation goes
+// to the second product as bf16 rows in expert order (s of them against h of an output row).
 #include "more_experts.cuh"
 
 namespace more {
 
 namespace {
 
-constexpr int kXThreads = 320;                       // warps 0, 1: TMA, MMA; warps 2..9: epilogue
-constexpr int kGatherWarps = 4;                      // ... and, where rows are gathered, warps 10..13
-constexpr int kXGatherThreads = kXThreads + kGatherWarps * 32;
-constexpr int kXRing = 160 * 1024;
-constexpr int kXStaging = 64 * 1024;                 // what the epilogue passes from the tensor memory's layout to memory's
-constexpr int kXSmem = kXRing + kXStaging + 1024 /*alignment*/ + 1024 /*barriers*/;
-constexpr int kXMaxStages = 12;
+// Warp 1 issues the MMAs, warps 2..9 are the epilogue, warp 0 and those from 10 on load: stage n is the (n mod loaders)th one's, as
+// opening a stage and issuing its loads costs a warp 700 to 3000 clocks, several times what a stage may take.
+constexpr int kLoaders = 5, kFewLoaders = 3;         // where rows are gathered; elsewhere
+constexpr int threads_of(int loaders) { return (9 + loaders) * 32; }
+__device__ __forceinline__ int loader_of(int warp) { return warp == 0 ? 0 : warp - 9; }
 constexpr int kTileRows = 128;
-constexpr int kATile = kTileRows * 128;              // 128 rows of 64 bf16
 constexpr int kBox = 64 * 128;                       // 64 rows of 64 bf16
+constexpr int kRowPitch = 528;                       // a staged output row: 256 16-bit values, and 16 bytes so that rows fall on other banks
+constexpr int kXStaging = kTileRows * kRowPitch;     // what the epilogue passes from the tensor memory's layout to memory's
+constexpr int kXRing = 154 * 1024;
+constexpr int kXControl = 1024 + kLoaders * 512;
+constexpr int kXSmem = kXRing + kXStaging + 1024 /*alignment*/ + kXControl;
+static_assert(kXSmem <= 227 * 1024, "shared memory");
+static_assert(kXStaging >= kTileRows * 128, "an operand of fewer rows than the MMA's 128 is read past its end");
+constexpr int kSlots = 16;                           // stages in flight at most
 
 enum { kUp = 0, kDown = 1, kBackAct = 2, kBackX = 3 };
 
 // Loads as a converged warp issues them: every lane passes the same operands and elect.sync picks the lane that issues.  (The
-// instructions take their operands from uniform registers; behind a branch that one lane takes each cost ~150 clocks to issue,
-// in this form a fraction of that.)
-// Up to four gathers of four rows each, `step` bytes of shared memory apart, as many as `count` says.
-__device__ __forceinline__ void tma_gather4x4(uint32_t dst, uint32_t step, const CUtensorMap* map, uint32_t bar, int x, int count, const int (&r)[16])
-{
-    asm volatile(
-        "{\n\t.reg .pred pe, p0, p1, p2, p3;\n\t.reg .b32 d1, d2, d3;\n\t"
-        "elect.sync _|pe, 0xffffffff;\n\t"
-        "setp.gt.and.s32 p0, %5, 0, pe;\n\tsetp.gt.and.s32 p1, %5, 1, pe;\n\tsetp.gt.and.s32 p2, %5, 2, pe;\n\tsetp.gt.and.s32 p3, %5, 3, pe;\n\t"
-        "add.u32 d1, %0, %1;\n\tadd.u32 d2, d1, %1;\n\tadd.u32 d3, d2, %1;\n\t"
-        "@p0 cp.async.bulk.tensor.2d.shared::cta.global.tile::gather4.mbarrier::complete_tx::bytes [%0], [%2, {%4, %6, %7, %8, %9}], [%3];\n\t"
-        "@p1 cp.async.bulk.tensor.2d.shared::cta.global.tile::gather4.mbarrier::complete_tx::bytes [d1], [%2, {%4, %10, %11, %12, %13}], [%3];\n\t"
-        "@p2 cp.async.bulk.tensor.2d.shared::cta.global.tile::gather4.mbarrier::complete_tx::bytes [d2], [%2, {%4, %14, %15, %16, %17}], [%3];\n\t"
-        "@p3 cp.async.bulk.tensor.2d.shared::cta.global.tile::gather4.mbarrier::complete_tx::bytes [d3], [%2, {%4, %18, %19, %20, %21}], [%3];\n\t}"
-        ::"r"(dst), "r"(step), "l"(map), "r"(bar), "r"(x), "r"(count), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]),
-          "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
-        : "memory");
-}
+// instructions take their operands from uniform registers; behind a branch that one lane takes each costs ~150 clocks to issue.)
 __device__ __forceinline__ void tma_load_2d_elect(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1)
 {
     asm volatile(
@@ -79,6 +71,32 @@ __device__ __forceinline__ void expect_elect(uint32_t bar, uint32_t bytes)
         "{\n\t.reg .pred pe;\n\telect.sync _|pe, 0xffffffff;\n\t"
         "@pe mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n\t}" ::"r"(bar), "r"(bytes) : "memory");
 }
+// Up to four gathers of four rows each, 512 bytes of shared memory apart, as many as `count` says.
+__device__ __forceinline__ void tma_gather16(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int count, int4 a, int4 b, int4 c, int4 d)
+{
+    asm volatile(
+        "{\n\t.reg .pred pe, p0, p1, p2, p3;\n\t.reg .b32 d1, d2, d3;\n\t"
+        "elect.sync _|pe, 0xffffffff;\n\t"
+        "setp.gt.and.s32 p0, %4, 0, pe;\n\tsetp.gt.and.s32 p1, %4, 1, pe;\n\tsetp.gt.and.s32 p2, %4, 2, pe;\n\tsetp.gt.and.s32 p3, %4, 3, pe;\n\t"
+        "add.u32 d1, %0, 512;\n\tadd.u32 d2, %0, 1024;\n\tadd.u32 d3, %0, 1536;\n\t"
+        "@p0 cp.async.bulk.tensor.2d.shared::cta.global.tile::gather4.mbarrier::complete_tx::bytes [%0], [%1, {%3, %5, %6, %7, %8}], [%2];\n\t"
+        "@p1 cp.async.bulk.tensor.2d.shared::cta.global.tile::gather4.mbarrier::complete_tx::bytes [d1], [%1, {%3, %9, %10, %11, %12}], [%2];\n\t"
+        "@p2 cp.async.bulk.tensor.2d.shared::cta.global.tile::gather4.mbarrier::complete_tx::bytes [d2], [%1, {%3, %13, %14, %15, %16}], [%2];\n\t"
+        "@p3 cp.async.bulk.tensor.2d.shared::cta.global.tile::gather4.mbarrier::complete_tx::bytes [d3], [%1, {%3, %17, %18, %19, %20}], [%2];\n\t}"
+        ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(count), "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b.x), "r"(b.y), "r"(b.z), "r"(b.w),
+          "r"(c.x), "r"(c.y), "r"(c.z), "r"(c.w), "r"(d.x), "r"(d.y), "r"(d.z), "r"(d.w)
+        : "memory");
+}
+// Stores that read shared memory by themselves; commit and wait by the thread that issued them.
+__device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, uint32_t src, int c0, int c1, int c2)
+{
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(map), "r"(src), "r"(c0), "r"(c1),
+                 "r"(c2) : "memory");
+}
+__device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void bulk_read_done() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory"); }   // all but the last N have read
+__device__ __forceinline__ void bulk_all_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 
 // Instruction descriptor of umma_idesc with the operands' majors: fp32 += bf16 x bf16, 128 rows, n columns.
 __device__ __forceinline__ uint32_t idesc_of(int n, int a_mn, int b_mn)
@@ -86,6 +104,62 @@ __device__ __forceinline__ uint32_t idesc_of(int n, int a_mn, int b_mn)
     return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) | ((uint32_t)(n >> 3) << 17) |
            ((uint32_t)(128 >> 4) << 24);
 }
+// A value requested ahead: what is computed from it stays behind this point (otherwise it is computed, and waited for, at once).
+__device__ __forceinline__ int hold(int v)
+{
+    asm volatile("" : "+r"(v));
+    return v;
+}
+
+struct Control {
+    uint64_t full[kSlots], empty[kSlots], acc_full[2], acc_empty[2];
+    uint32_t tmem;
+    int abort;
+    int pair[kTileRows];
+    int4 rows[kLoaders][kTileRows / 4];   // of each loader's tile
+};
+static_assert(sizeof(Control) <= kXControl, "control block");
+
+// The ring of stages, each as long as what it holds (a multiple of 1024 bytes).  Every loader, and the warp that empties it, goes
+// through the same sequence of lengths and so knows where each stage lies.
+struct Ring {
+    uint32_t head = 0;                    // next free byte
+    uint32_t end = 0;                     // bytes of all stages so far, gaps at the ring's end included
+    int n = 0;                            // stages so far
+    uint32_t begun = 0;                   // lane i < 16: `end` at which the last stage of slot i began
+    // Where the next stage of that length lies; `from`: the value of `end` in front of it.
+    __device__ uint32_t place(uint32_t bytes, uint32_t* from)
+    {
+        const bool wraps = head + bytes > (uint32_t)kXRing;
+        const uint32_t at = wraps ? 0u : head;
+        *from = end;
+        end += bytes + (wraps ? (uint32_t)kXRing - head : 0u);
+        head = at + bytes;
+        return at;
+    }
+    // A loader's view of the next stage: true if it is its own and open, at *at.  (*live: false if the CTA is giving up.)
+    __device__ bool open(uint32_t bytes, int loader, int loaders, Control* c, int lane, volatile int* abort_flag, int* status, uint32_t* at, bool* live)
+    {
+        uint32_t from;
+        *at = place(bytes, &from);
+        const bool own = n % loaders == loader;
+        if (own) {
+            // Of the last 16 stages those that began more than a ring's length before this one's end have to be empty, and the
+            // one whose slot this is (a slot that had none yet counts as one of long ago); they are emptied in order.
+            const unsigned old = __ballot_sync(0xffffffffu, lane < kSlots && (lane >= n || lane == n % kSlots || (int)(end - (uint32_t)kXRing - begun) > 0));
+            const int last = n - kSlots + __popc(old) - 1;
+            if (last >= 0 && !mbar_wait(smem_u32(&c->empty[last % kSlots]), (last / kSlots) & 1, abort_flag, status)) {
+                *live = false;
+                return false;
+            }
+            __syncwarp();
+        }
+        if (lane == n % kSlots) begun = from;
+        return own;
+    }
+    __device__ int slot() const { return n % kSlots; }
+    __device__ uint32_t parity() const { return (uint32_t)(n / kSlots) & 1u; }
+};
 
 // ------------------------------------------------------------------------------------------------ tiles
 // One entry per tile of up to 128 consecutive places of one expert: (expert, first place, places, 0), experts ascending.
@@ -123,84 +197,53 @@ __global__ void __launch_bounds__(1024) tiles_kernel(const int32_t* __restrict__
     if (e == M - 1) tiles[0].x = min(at + mine, capacity);
 }
 
-struct RowsParams {
-    const int4* tiles;
-    const int32_t* pairs;
-    int P, k, h, s;
-    int rows;                     // of A's tensor: the row that is out of its bounds
-    int nb;                       // boxes of 64 weight columns per unit
-    int chunks;                   // units per tile
-    int ksteps;                   // of 64
-    int stages;
-    __nv_bfloat16* out;           // kUp: activation [P][s]; kDown: Y [P][h]
-    __nv_bfloat16* hidden;        // kUp: nullable; kBackAct: read
-    const float* gate;            // kBackAct
-    __nv_bfloat16* du;            // kBackAct: [P][2s]
-    __nv_bfloat16* ga;            // kBackAct: gate a, [P][s]
-    float* dgate_part;            // kBackAct: [chunks][P]
-    __half* dx;                   // kBackX: [P][h] scaled
-    float* dx_scale;              // kBackX: [P][dx_groups], a power of two per 128 columns
-    int dx_groups;
-    int* status;
-};
-
-struct Control {
-    uint64_t full[kXMaxStages], empty[kXMaxStages], acc_full[2], acc_empty[2];
-    uint32_t tmem;
-    int abort;
-    int pair[kTileRows];
-};
-static_assert(sizeof(Control) <= 1024, "control block");
-
 // Barrier of the eight epilogue warps.
 __device__ __forceinline__ void epilogue_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
 
-// Staging: rows of `pitch` bytes, a power of two; the 16-byte pieces of a row are permuted by the row's number, so that neither a
-// warp that writes a piece of 32 rows nor one that reads along a row meets itself on a bank.
+__device__ __forceinline__ void st_piece(uint32_t at, uint4 v)
+{
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+// (Not volatile: several may be in flight.  The barriers around them keep them in their place.)
+__device__ __forceinline__ uint4 ld_piece(const uint8_t* at) { return *reinterpret_cast<const uint4*>(at); }
+// fp32 staging: rows of `pitch` bytes, a power of two; the 16-byte pieces of a row are permuted by the row's number, so that neither
+// a warp that writes a piece of 32 rows nor one that reads along a row meets itself on a bank.
 __device__ __forceinline__ uint32_t staged(uint32_t base, int pitch, int row, int piece) { return base + row * pitch + ((piece ^ (row & 7)) << 4); }
-__device__ __forceinline__ void st_piece(uint32_t at, uint32_t a, uint32_t b, uint32_t c, uint32_t d)
-{
-    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
-}
-__device__ __forceinline__ uint4 ld_piece(uint32_t at)
-{
-    uint4 v;
-    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
-    return v;
-}
-// 16 fp32 of a row into staging, from piece `piece` on; 32 values as bf16.
 __device__ __forceinline__ void stage_f32(uint32_t base, int pitch, int row, int piece, const float (&v)[16])
 {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-        st_piece(staged(base, pitch, row, piece + i), __float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]), __float_as_uint(v[4 * i + 2]),
-                 __float_as_uint(v[4 * i + 3]));
+        st_piece(staged(base, pitch, row, piece + i), make_uint4(__float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]),
+                                                                 __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3])));
 }
-__device__ __forceinline__ void stage_bf16(uint32_t base, int pitch, int row, int piece, const float (&v)[16])
+__device__ __forceinline__ void unstage8(const uint8_t* base, int pitch, int row, int piece, float (&v)[8])
 {
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-        st_piece(staged(base, pitch, row, piece + i), pack_bf16(v[8 * i], v[8 * i + 1]), pack_bf16(v[8 * i + 2], v[8 * i + 3]),
-                 pack_bf16(v[8 * i + 4], v[8 * i + 5]), pack_bf16(v[8 * i + 6], v[8 * i + 7]));
-}
-// 8 fp32 of a row, two pieces.
-__device__ __forceinline__ void unstage8(uint32_t base, int pitch, int row, int piece, float (&v)[8])
-{
-    const uint4 a = ld_piece(staged(base, pitch, row, piece)), b = ld_piece(staged(base, pitch, row, piece + 1));
+    const uint4 a = ld_piece(base + staged(0, pitch, row, piece)), b = ld_piece(base + staged(0, pitch, row, piece + 1));
     v[0] = __uint_as_float(a.x); v[1] = __uint_as_float(a.y); v[2] = __uint_as_float(a.z); v[3] = __uint_as_float(a.w);
     v[4] = __uint_as_float(b.x); v[5] = __uint_as_float(b.y); v[6] = __uint_as_float(b.z); v[7] = __uint_as_float(b.w);
 }
-__device__ __forceinline__ uint4 pack8(const float (&v)[8])
+template <int N>
+__device__ __forceinline__ uint4 pack8(const float (&v)[N], int at = 0)
 {
-    return make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+    return make_uint4(pack_bf16(v[at], v[at + 1]), pack_bf16(v[at + 2], v[at + 3]), pack_bf16(v[at + 4], v[at + 5]), pack_bf16(v[at + 6], v[at + 7]));
+}
+__device__ __forceinline__ uint4 pack8_half(const float (&v)[16], int at, float scale)
+{
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const __half2 q = __floats2half2_rn(v[at + 2 * i] * scale, v[at + 2 * i + 1] * scale);
+        w[i] = *reinterpret_cast<const uint32_t*>(&q);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
 // Common start of both kernels: barriers, tensor memory.  Returns the tensor-memory base.
-__device__ __forceinline__ uint32_t open_cta(Control* c, int stages, int producers, int warp)
+__device__ __forceinline__ uint32_t open_cta(Control* c, int warp)
 {
     if (threadIdx.x == 0) {
-        for (int i = 0; i < stages; ++i) {
-            mbar_init(smem_u32(&c->full[i]), producers);
+        for (int i = 0; i < kSlots; ++i) {
+            mbar_init(smem_u32(&c->full[i]), 1);
             mbar_init(smem_u32(&c->empty[i]), 1);
         }
         for (int i = 0; i < 2; ++i) {
@@ -232,158 +275,201 @@ __device__ __forceinline__ void close_cta(Control* c, uint32_t tmem, int warp)
     }
 }
 
-// The tiles of a CTA's units in turn, and the pair in place `r` of each: a unit's pair is requested a unit ahead, its tile two.
+// Division of 0 ... 2^31 - 1 by a small number: with 2^s >= d, m = ceil(2^(31 + s) / d) < 2^32, n / d = n m >> (31 + s) (the excess
+// n (m d - 2^(31 + s)) / (d 2^(31 + s)) < 2^31 d / (d 2^(31 + s)) = 2^-s <= 1 / d is never enough to reach the next quotient).
+struct Divide {
+    uint32_t m;
+    int shift;
+    __host__ void by(int d)
+    {
+        int s = 0;
+        while ((1 << s) < d) ++s;
+        shift = 31 + s;
+        m = (uint32_t)(((1ull << shift) + (unsigned)d - 1) / (unsigned)d);
+    }
+    __device__ int operator()(int n) const { return (int)((unsigned long long)(uint32_t)n * m >> shift); }
+};
+
+struct RowsParams {
+    const int4* tiles;
+    const int32_t* pairs;
+    int P, h, s;
+    Divide by_k;                  // pair -> token
+    int rows;                     // of A's tensor: the row that is out of its bounds
+    int nb;                       // boxes of 64 weight columns per unit
+    int chunks;                   // units per tile
+    int ksteps;                   // of 64
+    __nv_bfloat16* out;           // kUp: activation [P][s]; kDown: Y [P][h]
+    __nv_bfloat16* hidden;        // kUp: nullable; kBackAct: read
+    const float* gate;            // kBackAct
+    __nv_bfloat16* du;            // kBackAct: [P][2s]
+    __nv_bfloat16* ga;            // kBackAct: gate a, [P][s], nullable
+    float* dgate_part;            // kBackAct: [chunks][P]
+    __half* dx;                   // kBackX: [P][h] scaled
+    uint8_t* dx_scale;            // kBackX: [P][dx_groups], a power of two per 32 columns, as fp32's exponent
+    int dx_groups;
+    int* status;
+};
+
+// The tiles of a CTA's units in turn, and the pairs in N places r, r + 32, ... of each: a unit's pairs are requested a unit ahead, its
+// tile two.
+template <int N>
 struct TilesAhead {
     const RowsParams& p;
-    int units, r, pair, next_pair;
-    int4 tile, next_tile, last_tile;
-    __device__ TilesAhead(const RowsParams& q, int n, int row) : p(q), units(n), r(row), pair(-1), next_pair(-1)
+    int units, r, next_pair[N];
+    int step_tile, step_chunk, at_tile, at_chunk;            // units between a CTA's, as tiles and chunks; those of the unit after the next
+    int4 next_tile, last_tile;
+    int unit, chunk, next_chunk, pair[N];
+    int4 tile;
+    __device__ TilesAhead(const RowsParams& q, int n, int row) : p(q), units(n), r(row), unit((int)blockIdx.x - (int)gridDim.x)
     {
-        tile = next_tile = last_tile = make_int4(0, 0, 0, 0);
-        if ((int)blockIdx.x < units) tile = p.tiles[1 + blockIdx.x / p.chunks];
-        if ((int)(blockIdx.x + gridDim.x) < units) next_tile = p.tiles[1 + (blockIdx.x + gridDim.x) / p.chunks];
-        if (r < tile.z) pair = p.pairs[tile.y + r];
-        ask(blockIdx.x);
+        step_tile = (int)gridDim.x / p.chunks;
+        step_chunk = (int)gridDim.x % p.chunks;
+        at_tile = (int)blockIdx.x / p.chunks;
+        at_chunk = (int)blockIdx.x % p.chunks;
+        next_chunk = chunk = at_chunk;
+        next_tile = last_tile = make_int4(0, 0, 0, 0);
+        if ((int)blockIdx.x < units) next_tile = p.tiles[1 + at_tile];
+        advance();
+        if ((int)(blockIdx.x + gridDim.x) < units) last_tile = p.tiles[1 + at_tile];
+        ask_pairs();
+        next();
     }
-    __device__ void ask(int unit)
+    __device__ void advance()
     {
-        next_pair = r < next_tile.z ? p.pairs[next_tile.y + r] : -1;
+        at_tile += step_tile;
+        at_chunk += step_chunk;
+        if (at_chunk >= p.chunks) {
+            at_chunk -= p.chunks;
+            ++at_tile;
+        }
+    }
+    __device__ void ask_pairs()
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) next_pair[i] = r + 32 * i < next_tile.z ? p.pairs[next_tile.y + r + 32 * i] : -1;
+    }
+    __device__ bool more() const { return unit < units; }
+    __device__ void next()
+    {
+        unit += gridDim.x;
+        chunk = next_chunk;
+        next_chunk = at_chunk;
+        tile = make_int4(hold(next_tile.x), hold(next_tile.y), hold(next_tile.z), 0);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            pair[i] = hold(next_pair[i]);
+            if (pair[i] >= p.P) pair[i] = -1;
+        }
+        next_tile = make_int4(hold(last_tile.x), hold(last_tile.y), hold(last_tile.z), 0);
+        if constexpr (N > 0) ask_pairs();
         last_tile = make_int4(0, 0, 0, 0);
-        const long long u = unit + 2ll * gridDim.x;
-        if (u < units) last_tile = p.tiles[1 + (int)u / p.chunks];
-    }
-    __device__ void next(int unit)                          // after `unit`
-    {
-        tile = next_tile;
-        pair = next_pair;
-        next_tile = last_tile;
-        ask(unit + gridDim.x);
+        advance();
+        if (unit < units - 2 * (int)gridDim.x) last_tile = p.tiles[1 + at_tile];
     }
 };
 
+// Bytes of the rows of a tile, 64 columns, in a stage: gathered rows as many groups of eight as there are, others all 128 by boxes of 32.
+template <bool GATHER>
+__device__ __forceinline__ uint32_t row_bytes(int rows) { return GATHER ? (uint32_t)(rows + 7) / 8 * 1024 : 4u * 4096; }
+// Those 128 are the rows of the tile once, or a tile of up to 64 twice, up to 32 four times: each lane quarter of the accumulator is
+// read by warps of its own, which then share the columns.  How many of the four boxes differ:
+__device__ __forceinline__ int unlike_boxes(int rows) { return rows <= 32 ? 1 : rows <= 64 ? 2 : 4; }
+
 template <int MODE>
-__global__ void __launch_bounds__(MODE == kUp || MODE == kBackAct ? kXGatherThreads : kXThreads, 1)
+__global__ void __launch_bounds__(threads_of(MODE == kUp || MODE == kBackAct ? kLoaders : kFewLoaders), 1)
 rows_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUtensorMap mw, const __grid_constant__ RowsParams p)
 {
-    constexpr bool kByToken = MODE == kUp || MODE == kBackAct;      // rows of A are tokens, else places in expert order
+    constexpr bool kGather = MODE == kUp || MODE == kBackAct;       // rows of A are tokens', else places in expert order
     constexpr bool kMn = MODE == kUp || MODE == kDown;              // weights as an MN-major operand
     extern __shared__ uint8_t smem_raw[];
     const uint32_t ring = (smem_u32(smem_raw) + 1023u) & ~1023u, staging = ring + kXRing;
-    Control* ctl = reinterpret_cast<Control*>(smem_raw + (ring - smem_u32(smem_raw)) + kXRing + kXStaging);
+    uint8_t* const staging_at = smem_raw + (ring - smem_u32(smem_raw)) + kXRing;
+    Control* ctl = reinterpret_cast<Control*>(staging_at + kXStaging);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t tmem = open_cta(ctl, p.stages, kByToken ? 1 + kGatherWarps : 1, warp);
+    const uint32_t tmem = open_cta(ctl, warp);
     volatile int* abort_flag = &ctl->abort;
     const int units = p.tiles[0].x * p.chunks;
-    const uint32_t stage_bytes = kATile + p.nb * kBox;
 
-    if (warp == 0) {
-        int stage = 0;
-        uint32_t phase = 0;
+    if (warp == 0 || warp >= 10) {
+        constexpr int kMine = kGather ? kLoaders : kFewLoaders;
+        const int loader = loader_of(warp);
+        int4* rows = ctl->rows[loader];
+        Ring rg;
         bool live = true;
-        int4 next = make_int4(0, 0, 0, 0);
-        if ((int)blockIdx.x < units) next = p.tiles[1 + blockIdx.x / p.chunks];
-        for (int unit = blockIdx.x; unit < units && live; unit += gridDim.x) {
-            const int4 tile = next;
-            if (unit + (int)gridDim.x < units) next = p.tiles[1 + (unit + gridDim.x) / p.chunks];
-            const int chunk = unit % p.chunks, boxes = kByToken ? 0 : (tile.z + 31) / 32;
-            for (int ks = 0; ks < p.ksteps; ++ks) {
-                const uint32_t full = smem_u32(&ctl->full[stage]);
-                if (!mbar_wait(smem_u32(&ctl->empty[stage]), phase ^ 1u, abort_flag, p.status)) { live = false; break; }
-                const uint32_t at = ring + stage * stage_bytes;
-                __syncwarp();
-                expect_elect(full, boxes * 4096 + p.nb * kBox);
-                for (int b = 0; b < p.nb; ++b) {
-                    int x, y;
-                    if (MODE == kUp) {
-                        const int half = p.nb / 2;
-                        x = (b < half ? 0 : p.s) + (chunk * half + (b < half ? b : b - half)) * 64;
-                        y = ks * 64;
-                    } else if (kMn) {
-                        x = (chunk * p.nb + b) * 64;
-                        y = ks * 64;
-                    } else {
-                        x = ks * 64;
-                        y = (chunk * p.nb + b) * 64;
-                    }
-                    tma_load_3d_elect(at + kATile + b * kBox, &mw, full, x, y, tile.x);
-                }
-                for (int b = 0; b < boxes; ++b) tma_load_2d_elect(at + b * 4096, &ma, full, ks * 64, tile.y + b * 32);
-                if (++stage == p.stages) { stage = 0; phase ^= 1u; }
-            }
-        }
-    } else if (kByToken && warp >= 10) {
-        // Rows 16 i + 4 w .. + 3 of the tile for i = 0, 1, ... are warp w's: up to eight gathers a step.
-        const int r0 = (warp - 10) * 4;
-        int stage = 0;
-        uint32_t phase = 0;
-        bool live = true;
-        const int r = (lane >> 2) * 16 + r0 + (lane & 3);
-        TilesAhead ahead(p, units, r);
-        for (int unit = blockIdx.x; unit < units && live; unit += gridDim.x) {
-            const int gathers = (max(0, ahead.tile.z - r0) + 15) / 16;
-            const int mine = ahead.pair < 0 || ahead.pair >= p.P ? p.rows : (int)((unsigned)ahead.pair / (unsigned)p.k);    // (no such row: out of bounds, zeros)
-            int lo[16], hi[16];
+        for (TilesAhead<kGather ? 4 : 0> u(p, units, lane); u.more() && live; u.next()) {
+            const uint32_t a_bytes = row_bytes<kGather>(u.tile.z), bytes = a_bytes + p.nb * kBox;
+            const int gathers = (u.tile.z + 3) / 4, unlike = unlike_boxes(u.tile.z);
+            if constexpr (kGather) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                lo[i] = __shfl_sync(0xffffffffu, mine, i);
-                hi[i] = __shfl_sync(0xffffffffu, mine, 16 + i);
-            }
-            ahead.next(unit);
-            for (int ks = 0; ks < p.ksteps; ++ks) {
-                const uint32_t full = smem_u32(&ctl->full[stage]);
-                if (!mbar_wait(smem_u32(&ctl->empty[stage]), phase ^ 1u, abort_flag, p.status)) { live = false; break; }
-                const uint32_t at = ring + stage * stage_bytes + r0 * 128;
+                for (int i = 0; i < 4; ++i)                         // (a row that does not exist is out of bounds: zeros)
+                    reinterpret_cast<int*>(rows)[i * 32 + lane] = u.pair[i] < 0 ? p.rows : p.by_k(u.pair[i]);
                 __syncwarp();
-                expect_elect(full, gathers * 512);
-                tma_gather4x4(at, 2048, &ma, full, ks * 64, gathers, lo);
-                if (gathers > 4) tma_gather4x4(at + 8192, 2048, &ma, full, ks * 64, gathers - 4, hi);
-                if (++stage == p.stages) { stage = 0; phase ^= 1u; }
             }
+            for (int ks = 0; ks < p.ksteps && live; ++ks, ++rg.n) {
+                uint32_t at;
+                if (!rg.open(bytes, loader, kMine, ctl, lane, abort_flag, p.status, &at, &live)) continue;
+                const uint32_t full = smem_u32(&ctl->full[rg.slot()]);
+                at += ring;
+                expect_elect(full, (kGather ? gathers * 512 : a_bytes) + p.nb * kBox);
+                if constexpr (kMn) {
+                    for (int b = 0; b < p.nb; ++b) {
+                        const int half = p.nb / 2;
+                        const int x = MODE == kDown ? (u.chunk * p.nb + b) * 64 : (b < half ? 0 : p.s) + (u.chunk * half + (b < half ? b : b - half)) * 64;
+                        tma_load_3d_elect(at + a_bytes + b * kBox, &mw, full, x, ks * 64, u.tile.x);
+                    }
+                } else {
+                    tma_load_3d_elect(at + a_bytes, &mw, full, ks * 64, u.chunk * p.nb * 64, u.tile.x);
+                }
+                if constexpr (kGather) {
+                    for (int g = 0; g < gathers; g += 4)
+                        tma_gather16(at + g * 512, &ma, full, ks * 64, gathers - g, rows[g], rows[g + 1], rows[g + 2], rows[g + 3]);
+                } else {
+                    for (int b = 0; b < 4; ++b) tma_load_2d_elect(at + b * 4096, &ma, full, ks * 64, u.tile.y + (b & (unlike - 1)) * 32);
+                }
+            }
+            __syncwarp();                                           // (the rows are read)
         }
     } else if (warp == 1) {
         const uint32_t idesc = idesc_of(p.nb * 64, 0, kMn);
-        const uint64_t a0 = umma_desc_sw128(ring, 16, 1024);
-        const uint64_t b0 = kMn ? umma_desc_sw128(ring + kATile, kBox, 1024) : umma_desc_sw128(ring + kATile, 16, 1024);
+        const uint64_t a0 = umma_desc_sw128(ring, 16, 1024), b0 = umma_desc_sw128(ring, kMn ? kBox : 16, 1024);
         const uint32_t a_hi = (uint32_t)(a0 >> 32), b_hi = (uint32_t)(b0 >> 32);
         constexpr uint32_t kBStep = kMn ? 2048 >> 4 : 32 >> 4;
-        int stage = 0, it = 0;
-        uint32_t phase = 0;
+        Ring rg;
+        int it = 0;
         bool live = true;
-        for (int unit = blockIdx.x; unit < units && live; unit += gridDim.x, ++it) {
+        for (TilesAhead<0> u(p, units, 0); u.more() && live; u.next(), ++it) {
             const int buf = it & 1;
+            const uint32_t a_bytes = row_bytes<kGather>(u.tile.z), bytes = a_bytes + p.nb * kBox;
             if (!mbar_wait(smem_u32(&ctl->acc_empty[buf]), ((it >> 1) & 1) ^ 1u, abort_flag, p.status)) break;
             tc_fence_after();
             for (int ks = 0; ks < p.ksteps; ++ks) {
-                if (!mbar_wait(smem_u32(&ctl->full[stage]), phase, abort_flag, p.status)) { live = false; break; }
+                uint32_t from;
+                const uint32_t off = rg.place(bytes, &from);
+                if (!mbar_wait(smem_u32(&ctl->full[rg.slot()]), rg.parity(), abort_flag, p.status)) { live = false; break; }
                 tc_fence_after();
-                const uint32_t off = (stage * stage_bytes) >> 4;
+                const uint32_t al = (uint32_t)a0 + (off >> 4), bl = (uint32_t)b0 + ((off + a_bytes) >> 4);
 #pragma unroll
                 for (int q = 0; q < 4; ++q)
-                    tc_mma_bf16_ss_elect(tmem + buf * 256, (uint32_t)a0 + off + q * 2, a_hi, (uint32_t)b0 + off + q * kBStep, b_hi, idesc,
-                                         ks > 0 || q > 0);
-                tc_commit_elect(smem_u32(&ctl->empty[stage]));
-                if (++stage == p.stages) { stage = 0; phase ^= 1u; }
+                    tc_mma_bf16_ss_elect(tmem + buf * 256, al + q * 2, a_hi, bl + q * kBStep, b_hi, idesc, ks > 0 || q > 0);
+                tc_commit_elect(smem_u32(&ctl->empty[rg.slot()]));
+                ++rg.n;
             }
             if (live) tc_commit_elect(smem_u32(&ctl->acc_full[buf]));
         }
-    } else if (warp < 10) {
-        // Two steps per pass: the warps that have rows copy columns of the accumulator into staging, thread by row; then all
-        // eight work along rows, so that memory is read and written in whole lines and a tile of few rows occupies them all.
+    } else {
+        // The accumulator comes thread by row; memory is written along rows, so values pass through staging.  Where there is work to
+        // be done on them (kUp, kBackAct) all eight warps do it along rows, so that a tile of few rows occupies them all; where
+        // they are only rounded, each warp handles its own rows and columns and waits for nobody.
         const int quarter = warp & 3, side = warp >= 6;             // lane quarter of the accumulator; half of the columns
         const int r0 = quarter * 32, row = r0 + lane;               // this warp's first row of a tile, this thread's
         const int tid = threadIdx.x - 64;
-        constexpr int kPitch = MODE == kUp || MODE == kBackAct ? (MODE == kUp ? 512 : 256) : 512;
         int it = 0;
-        TilesAhead ahead(p, units, row);
-        for (int unit = blockIdx.x; unit < units; unit += gridDim.x, ++it) {
-            const int4 tile = ahead.tile;
-            const int chunk = unit % p.chunks, buf = it & 1;
-            const int my_pair = ahead.pair < p.P ? ahead.pair : -1;
-            if constexpr (MODE != kUp)
-                if (side == 0) ctl->pair[row] = my_pair;            // (read behind the first barrier below)
-            ahead.next(unit);
-            const uint32_t acc = tmem + buf * 256 + ((uint32_t)(quarter * 32) << 16);
-            // after a wait that gave up the loop goes on without work: no warp is left alone at a barrier
+        // (pairs: of row `row` in kBackAct, of row `tid` in the others' warps of the first half)
+        for (TilesAhead<MODE == kUp ? 0 : 1> u(p, units, MODE == kBackAct ? row : tid & 127); u.more(); u.next(), ++it) {
+            const int4 tile = u.tile;
+            const int chunk = u.chunk, buf = it & 1;
+            const uint32_t acc = tmem + buf * 256 + ((uint32_t)r0 << 16);
             uint4 kept[4][2];                                       // kBackAct: both projections of this thread's first items
             if constexpr (MODE == kBackAct) {
 #pragma unroll
@@ -396,11 +482,12 @@ rows_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUte
                     }
                 }
             }
+            // after a wait that gave up the loop goes on without work: no warp is left alone at a barrier
             const bool ok = mbar_wait(smem_u32(&ctl->acc_full[buf]), (it >> 1) & 1, abort_flag, p.status);
             tc_fence_after();
             const int rows = ok ? tile.z : 0;
             const bool any = r0 < rows;                             // (a warp whose rows are all behind the tile copies nothing)
-            auto release = [&]() {
+            auto release = [&]() {                                  // the accumulator may be filled again
                 tc_fence_before();
                 warp_arrive(smem_u32(&ctl->acc_empty[buf]), lane);
             };
@@ -414,7 +501,7 @@ rows_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUte
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
                             tmem_ld_wait16(v[i]);
-                            stage_f32(staging, kPitch, row, (i >= 2 ? 16 : 0) + side * 8 + (i & 1) * 4, v[i]);
+                            stage_f32(staging, 512, row, (i >= 2 ? 16 : 0) + side * 8 + (i & 1) * 4, v[i]);
                         }
                     }
                     if (pass == passes - 1) release();
@@ -422,22 +509,23 @@ rows_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUte
                     const int s0 = chunk * cols + pass * 64 + (tid & 7) * 8;
                     for (int r = tid >> 3; r < rows; r += 32) {
                         if (s0 >= p.s) continue;
-                        float g[8], u[8], a[8];
-                        unstage8(staging, kPitch, r, (tid & 7) * 2, g);
-                        unstage8(staging, kPitch, r, 16 + (tid & 7) * 2, u);
+                        float g[8], w[8], a[8];
+                        unstage8(staging_at, 512, r, (tid & 7) * 2, g);
+                        unstage8(staging_at, 512, r, 16 + (tid & 7) * 2, w);
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) a[i] = g[i] * sigmoidf(g[i]) * u[i];
+                        for (int i = 0; i < 8; ++i) a[i] = g[i] * sigmoidf(g[i]) * w[i];
                         const long long place = tile.y + r;
                         *reinterpret_cast<uint4*>(p.out + place * p.s + s0) = pack8(a);
                         if (p.hidden) {
                             *reinterpret_cast<uint4*>(p.hidden + place * 2 * p.s + s0) = pack8(g);
-                            *reinterpret_cast<uint4*>(p.hidden + place * 2 * p.s + p.s + s0) = pack8(u);
+                            *reinterpret_cast<uint4*>(p.hidden + place * 2 * p.s + p.s + s0) = pack8(w);
                         }
                     }
                     epilogue_sync();
                 }
             } else if constexpr (MODE == kBackAct) {
                 const int width = p.nb * 64, passes = (min(width, p.s - chunk * width) + 63) / 64;
+                if (side == 0) ctl->pair[row] = u.pair[0];          // (the last tile's have been read)
                 float dg[4] = {0.f, 0.f, 0.f, 0.f};
                 for (int pass = 0; pass < passes; ++pass) {
                     if (any) {
@@ -447,7 +535,7 @@ rows_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUte
 #pragma unroll
                         for (int i = 0; i < 2; ++i) {
                             tmem_ld_wait16(v[i]);
-                            stage_f32(staging, kPitch, row, side * 8 + i * 4, v[i]);
+                            stage_f32(staging, 256, row, side * 8 + i * 4, v[i]);
                         }
                     }
                     if (pass == passes - 1) release();
@@ -465,7 +553,7 @@ rows_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUte
                         const float gate = pair >= 0 ? p.gate[pair] : 0.f;
                         const uint32_t wg[4] = {hg.x, hg.y, hg.z, hg.w}, wu[4] = {hu.x, hu.y, hu.z, hu.w};
                         float c[8], out_g[8], out_u[8], out_a[8];
-                        unstage8(staging, kPitch, r, (tid & 7) * 2, c);
+                        unstage8(staging_at, 256, r, (tid & 7) * 2, c);
 #pragma unroll
                         for (int j = 0; j < 8; ++j) {
                             const float g = j & 1 ? bf16_hi(wg[j / 2]) : bf16_lo(wg[j / 2]), up = j & 1 ? bf16_hi(wu[j / 2]) : bf16_lo(wu[j / 2]);
@@ -479,7 +567,7 @@ rows_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUte
                         *reinterpret_cast<uint4*>(p.du + place * 2 * p.s + p.s + s0) = pack8(out_u);
                         if (p.ga) *reinterpret_cast<uint4*>(p.ga + place * p.s + s0) = pack8(out_a);
                     }
-                    epilogue_sync();
+                    if (pass < passes - 1) epilogue_sync();
                 }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {                       // the eight threads of a row
@@ -489,62 +577,57 @@ rows_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUte
                     const int pair = r < rows ? ctl->pair[r] : -1;
                     if ((tid & 7) == 0 && pair >= 0) p.dgate_part[(long long)chunk * p.P + pair] = dg[i];
                 }
-                epilogue_sync();                                    // (the pairs are read)
+                epilogue_sync();
             } else {
                 const int per = p.nb * 32, c0 = chunk * p.nb * 64;
-                if (any) {
-                    float up = 1.f;
-                    if constexpr (MODE == kBackX) {
-                        // The rows of the slots are added later: each `per` (128, where h > 128) columns of a row are kept in fp16
-                        // behind a power of two that brings their largest to [2^14, 2^15): an eighth of bf16's rounding for the
-                        // same bytes.
-                        float top = 0.f;
-                        for (int c = 0; c < per && c0 + side * per + c < p.h; c += 32) {
-                            float v0[16], v1[16];
-                            tmem_ld16(acc + side * per + c, v0);
-                            tmem_ld16(acc + side * per + c + 16, v1);
-                            tmem_ld_wait16(v0); tmem_ld_wait16(v1);
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) top = max3(top, fabsf(v0[i]), fabsf(v1[i]));
-                        }
-                        const int ex = max(15, __float_as_int(top) >> 23);
-                        up = ex < 255 ? __int_as_float((268 - ex) << 23) : 1.f;
-                        const float down = ex < 255 ? __int_as_float((ex - 14) << 23) : 1.f;
-                        if (my_pair >= 0 && c0 + side * per < p.h) p.dx_scale[(long long)my_pair * p.dx_groups + c0 / per + side] = down;
-                    }
-                    for (int c = 0; c < per && c0 + side * per + c < p.h; c += 32) {
+                const int unlike = unlike_boxes(tile.z), copy = quarter / unlike, mine = (quarter % unlike) * 32 + lane;
+                if (side == 0) ctl->pair[tid] = u.pair[0];          // (the last unit's have been read)
+                if ((quarter % unlike) * 32 < rows)
+                    for (int c = copy * 32; c < per && c0 + side * per + c < p.h; c += 4 / unlike * 32) {
                         float v[2][16];
+                        tmem_ld16(acc + side * per + c, v[0]);
+                        tmem_ld16(acc + side * per + c + 16, v[1]);
+                        tmem_ld_wait16(v[0]); tmem_ld_wait16(v[1]);
+                        const uint32_t to = staging + mine * kRowPitch + (side * per + c) * 2;
+                        if constexpr (MODE == kDown) {
+                            st_piece(to, pack8(v[0], 0)); st_piece(to + 16, pack8(v[0], 8));
+                            st_piece(to + 32, pack8(v[1], 0)); st_piece(to + 48, pack8(v[1], 8));
+                        } else {
+                            // The rows of the slots are added later: each 32 columns of a row are kept in fp16 behind a power of two
+                            // that brings their largest to [2^14, 2^15): an eighth of bf16's rounding for 3 % more bytes.
+                            // (Columns behind the row's end are zeros: there the weights are out of bounds.)
+                            float top = 0.f;
 #pragma unroll
-                        for (int i = 0; i < 2; ++i) tmem_ld16(acc + side * per + c + i * 16, v[i]);
-#pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            tmem_ld_wait16(v[i]);
-                            const int piece = (side * per + c + i * 16) / 8;
-                            if constexpr (MODE == kDown) {
-                                stage_bf16(staging, kPitch, row, piece, v[i]);
-                            } else {
-                                uint32_t w[8];
-#pragma unroll
-                                for (int j = 0; j < 8; ++j) {
-                                    const __half2 q = __floats2half2_rn(v[i][2 * j] * up, v[i][2 * j + 1] * up);
-                                    w[j] = *reinterpret_cast<const uint32_t*>(&q);
-                                }
-                                st_piece(staged(staging, kPitch, row, piece), w[0], w[1], w[2], w[3]);
-                                st_piece(staged(staging, kPitch, row, piece + 1), w[4], w[5], w[6], w[7]);
-                            }
+                            for (int i = 0; i < 16; ++i) top = max3(top, fabsf(v[0][i]), fabsf(v[1][i]));
+                            const int ex = max(15, __float_as_int(top) >> 23);
+                            const float up = ex < 255 ? __int_as_float((268 - ex) << 23) : 1.f;
+                            st_piece(to, pack8_half(v[0], 0, up)); st_piece(to + 16, pack8_half(v[0], 8, up));
+                            st_piece(to + 32, pack8_half(v[1], 0, up)); st_piece(to + 48, pack8_half(v[1], 8, up));
+                            staging_at[mine * kRowPitch + 512 + (side * per + c) / 32] = (uint8_t)(ex < 255 ? ex - 14 : 127);   // (behind the row)
                         }
                     }
-                }
                 release();
                 epilogue_sync();
                 // a warp per row: up to 512 consecutive bytes
                 uint16_t* out = MODE == kDown ? reinterpret_cast<uint16_t*>(p.out) : reinterpret_cast<uint16_t*>(p.dx);
                 const bool in = lane < p.nb * 8 && c0 + lane * 8 < p.h;
-#pragma unroll 4
-                for (int r = warp - 2; r < rows; r += 8) {
-                    const int pair = ctl->pair[r];
-                    const uint4 v = ld_piece(staged(staging, kPitch, r, lane));
-                    if (pair >= 0 && in) *reinterpret_cast<uint4*>(out + (long long)pair * p.h + c0 + lane * 8) = v;
+                for (int r = warp - 2; r < rows; r += 32) {
+                    uint4 v[4];
+                    int pair[4];
+                    uint8_t ex[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int q = min(r + 8 * i, kTileRows - 1);
+                        pair[i] = r + 8 * i < rows ? ctl->pair[q] : -1;
+                        v[i] = ld_piece(staging_at + q * kRowPitch + lane * 16);
+                        if (MODE == kBackX) ex[i] = staging_at[q * kRowPitch + 512 + (lane & 7)];
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        if (pair[i] < 0) continue;
+                        if (in) *reinterpret_cast<uint4*>(out + (long long)pair[i] * p.h + c0 + lane * 8) = v[i];
+                        if (MODE == kBackX && lane < p.nb * 2 && c0 + lane * 32 < p.h) p.dx_scale[(long long)pair[i] * p.dx_groups + c0 / 32 + lane] = ex[i];
+                    }
                 }
                 epilogue_sync();
             }
@@ -557,11 +640,11 @@ rows_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUte
 struct WeightsParams {
     const int32_t* offsets;
     const int32_t* pairs;
-    int P, T, k, M;
+    int P, T, M;
+    Divide by_k;
     int a_by_token;               // dW1: A = X by token, B = du by place; dW2: A = gate a by place, B = d by token
-    int rows, cols;               // of an expert's output
+    int rows, cols;               // of an expert's output: A's columns, B's columns
     int mtiles, chunks, nb;
-    int stages;
     __nv_bfloat16* out;           // [M][rows][cols]
     int* status;
 };
@@ -575,8 +658,9 @@ struct Units {
     int next_e, next_rem, raw_lo, raw_hi;
     __device__ explicit Units(const WeightsParams& q) : p(q), per_expert(q.mtiles * q.chunks), units((uint32_t)q.M * per_expert), unit(blockIdx.x)
     {
+        next_e = next_rem = raw_lo = raw_hi = 0;
         request();
-        take();
+        next();
     }
     __device__ void request()                               // (of the unit that `unit` names)
     {
@@ -586,166 +670,164 @@ struct Units {
         raw_lo = p.offsets[next_e];
         raw_hi = p.offsets[next_e + 1];
     }
-    __device__ void take()                                  // (whatever the offsets hold, a run stays within the places)
+    __device__ bool more() const { return unit - gridDim.x < units; }
+    __device__ void next()                                  // (whatever the offsets hold, a run stays within the places)
     {
         e = next_e;
         rem = next_rem;
-        lo = min(max(raw_lo, 0), p.P);
-        n = max(min(raw_hi, p.P) - lo, 0);
+        lo = min(max(hold(raw_lo), 0), p.P);
+        n = max(min(hold(raw_hi), p.P) - lo, 0);
         unit += gridDim.x;
         request();
     }
-    __device__ bool more() const { return unit - gridDim.x < units; }
-    __device__ void next() { take(); }
     __device__ int mtile() const { return p.chunks == 1 ? rem : rem / p.chunks; }
     __device__ int chunk() const { return p.chunks == 1 ? 0 : rem % p.chunks; }
 };
 
-__global__ void __launch_bounds__(kXGatherThreads, 1)
+__global__ void __launch_bounds__(threads_of(kLoaders), 1)
 weights_kernel(const __grid_constant__ CUtensorMap mtoken, const __grid_constant__ CUtensorMap mplace, const __grid_constant__ CUtensorMap mplace16,
-               const __grid_constant__ WeightsParams p)
+               const __grid_constant__ CUtensorMap mout, const __grid_constant__ WeightsParams p)
 {
     extern __shared__ uint8_t smem_raw[];
     const uint32_t ring = (smem_u32(smem_raw) + 1023u) & ~1023u, staging = ring + kXRing;
-    Control* ctl = reinterpret_cast<Control*>(smem_raw + (ring - smem_u32(smem_raw)) + kXRing + kXStaging);
+    uint8_t* const staging_at = smem_raw + (ring - smem_u32(smem_raw)) + kXRing;
+    Control* ctl = reinterpret_cast<Control*>(staging_at + kXStaging);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t tmem = open_cta(ctl, p.stages, kGatherWarps, warp);
+    const uint32_t tmem = open_cta(ctl, warp);
     volatile int* abort_flag = &ctl->abort;
-    const uint32_t stage_bytes = (2 + p.nb) * kBox;
 
-    if (warp >= 10) {
-        // Each of these warps loads 16 of a step's 64 rows, one K-step of the MMAs, of both operands: rows by token by gathers,
-        // consecutive places in one piece.  Rows behind the run's last are out of bounds, zeros: of the places, too, only then
-        // row by row (what lies there belongs to another expert).
-        const int part = warp - 10;
-        int stage = 0;
-        uint32_t phase = 0;
+    if (warp == 0 || warp >= 10) {
+        // A stage is up to 64 rows, as many whole MMA steps of 16 as it needs, of both operands' boxes of 64 columns: rows by token by
+        // gathers, consecutive places in pieces of 16.  Rows behind the run's last are out of bounds, zeros: of the places, too,
+        // only then row by row (what lies there belongs to another expert).
+        const int loader = loader_of(warp);
+        int4* rows = ctl->rows[loader];                             // 64 tokens, 64 places
+        Ring rg;
         bool live = true;
-        Units u(p);
-        while (u.more() && u.n == 0) u.next();
-        int at = 0, next_pair = -1;
-        auto fetch = [&]() {
-            const int r = at + part * 16 + (lane & 15);
-            next_pair = u.more() && r < u.n ? p.pairs[u.lo + r] : -1;
-        };
-        fetch();
-        while (u.more() && live) {
-            const int lo = u.lo, mt = u.mtile(), chunk = u.chunk(), r0 = at + part * 16, rows = min(16, u.n - r0);
-            const int a_boxes = p.rows - mt * 128 > 64 ? 2 : 1;
-            const bool in = next_pair >= 0 && next_pair < p.P;
-            const int mine = in ? (int)((unsigned)next_pair / (unsigned)p.k) : p.T;
-            const bool whole = __all_sync(0xffffffffu, in);
-            int token[16], place[16];
+        for (Units u(p); u.more() && live; u.next()) {
+            const int mt = u.mtile(), chunk = u.chunk(), a_boxes = p.rows - mt * 128 > 64 ? 2 : 1;
+            for (int at = 0; at < u.n && live; at += 64, ++rg.n) {
+                const int left = min(64, u.n - at), steps = (left + 15) / 16;
+                const uint32_t box = (uint32_t)steps * 2048;
+                uint32_t where;
+                if (rg.n % kLoaders == loader) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                token[i] = __shfl_sync(0xffffffffu, mine, i);
-                place[i] = token[i] == p.T ? p.P : lo + r0 + i;
-            }
-            at += 64;
-            if (at >= u.n) {
-                at = 0;
-                do u.next(); while (u.more() && u.n == 0);
-            }
-            fetch();
-            const uint32_t full = smem_u32(&ctl->full[stage]);
-            if (!mbar_wait(smem_u32(&ctl->empty[stage]), phase ^ 1u, abort_flag, p.status)) { live = false; break; }
-            const uint32_t base = ring + stage * stage_bytes + part * 2048;
-            __syncwarp();
-            expect_elect(full, rows > 0 ? 2048 * (a_boxes + p.nb) : 0);
-            if (rows > 0) {
+                    for (int i = 0; i < 2; ++i) {
+                        const int r = i * 32 + lane, place = u.lo + at + r, pair = r < left ? p.pairs[place] : -1;
+                        const bool in = pair >= 0 && pair < p.P;
+                        reinterpret_cast<int*>(rows)[r] = in ? p.by_k(pair) : p.T;
+                        reinterpret_cast<int*>(rows)[64 + r] = in ? place : p.P;
+                    }
+                    __syncwarp();
+                }
+                if (!rg.open(box * (a_boxes + p.nb), loader, kLoaders, ctl, lane, abort_flag, p.status, &where, &live)) continue;
+                const uint32_t full = smem_u32(&ctl->full[rg.slot()]);
+                expect_elect(full, box * (a_boxes + p.nb));
+                const uint32_t a_at = ring + where, b_at = a_at + a_boxes * box;
                 const int a_x = mt * 128, b_x = chunk * p.nb * 64;
-                const uint32_t a_at = base, b_at = base + 2 * kBox;
                 const int t_boxes = p.a_by_token ? a_boxes : p.nb, p_boxes = p.a_by_token ? p.nb : a_boxes;
                 const int t_x = p.a_by_token ? a_x : b_x, p_x = p.a_by_token ? b_x : a_x;
                 const uint32_t t_at = p.a_by_token ? a_at : b_at, p_at = p.a_by_token ? b_at : a_at;
-                for (int b = 0; b < t_boxes; ++b) tma_gather4x4(t_at + b * kBox, 512, &mtoken, full, t_x + b * 64, 4, token);
-                for (int b = 0; b < p_boxes; ++b) {
-                    if (whole) tma_load_2d_elect(p_at + b * kBox, &mplace16, full, p_x + b * 64, lo + r0);
-                    else tma_gather4x4(p_at + b * kBox, 512, &mplace, full, p_x + b * 64, 4, place);
+                for (int q = 0; q < steps; ++q) {
+                    const int4 r0 = rows[4 * q], r1 = rows[4 * q + 1], r2 = rows[4 * q + 2], r3 = rows[4 * q + 3];
+                    for (int b = 0; b < t_boxes; ++b) tma_gather16(t_at + b * box + q * 2048, &mtoken, full, t_x + b * 64, 4, r0, r1, r2, r3);
+                    if (left >= q * 16 + 16) {
+                        for (int b = 0; b < p_boxes; ++b) tma_load_2d_elect(p_at + b * box + q * 2048, &mplace16, full, p_x + b * 64, u.lo + at + q * 16);
+                    } else {
+                        const int4 s0 = rows[16 + 4 * q], s1 = rows[17 + 4 * q], s2 = rows[18 + 4 * q], s3 = rows[19 + 4 * q];
+                        for (int b = 0; b < p_boxes; ++b) tma_gather16(p_at + b * box + q * 2048, &mplace, full, p_x + b * 64, 4, s0, s1, s2, s3);
+                    }
                 }
+                __syncwarp();                                       // (the rows are read)
             }
-            if (++stage == p.stages) { stage = 0; phase ^= 1u; }
         }
     } else if (warp == 1) {
         const uint32_t idesc = idesc_of(p.nb * 64, 1, 1);
-        const uint64_t a0 = umma_desc_sw128(ring, kBox, 1024), b0 = umma_desc_sw128(ring + 2 * kBox, kBox, 1024);
-        const uint32_t a_hi = (uint32_t)(a0 >> 32), b_hi = (uint32_t)(b0 >> 32);
-        int stage = 0, it = 0;
-        uint32_t phase = 0;
+        const uint64_t d0 = umma_desc_sw128(ring, 0, 1024);
+        Ring rg;
+        int it = 0;
         bool live = true;
         for (Units u(p); u.more() && live; u.next()) {
             const int n = u.n;
             if (n == 0) continue;                                   // (the epilogue writes zeros without an accumulator)
-            const int buf = it & 1;
+            const int buf = it & 1, a_boxes = p.rows - u.mtile() * 128 > 64 ? 2 : 1;
             if (!mbar_wait(smem_u32(&ctl->acc_empty[buf]), ((it >> 1) & 1) ^ 1u, abort_flag, p.status)) break;
             tc_fence_after();
             for (int at = 0; at < n; at += 64) {
-                const int steps = (min(64, n - at) + 15) / 16;
-                if (!mbar_wait(smem_u32(&ctl->full[stage]), phase, abort_flag, p.status)) { live = false; break; }
+                const uint32_t steps = (min(64, n - at) + 15) / 16, box = steps * 2048;
+                uint32_t from;
+                const uint32_t off = rg.place(box * (a_boxes + p.nb), &from);
+                if (!mbar_wait(smem_u32(&ctl->full[rg.slot()]), rg.parity(), abort_flag, p.status)) { live = false; break; }
                 tc_fence_after();
-                const uint32_t off = (stage * stage_bytes) >> 4;
-                for (int q = 0; q < steps; ++q)
-                    tc_mma_bf16_ss_elect(tmem + buf * 256, (uint32_t)a0 + off + q * 128, a_hi, (uint32_t)b0 + off + q * 128, b_hi, idesc,
-                                         at > 0 || q > 0);
-                tc_commit_elect(smem_u32(&ctl->empty[stage]));
-                if (++stage == p.stages) { stage = 0; phase ^= 1u; }
+                // boxes lie `box` apart: the distance of 64 columns in both descriptors
+                const uint32_t a_lo = ((uint32_t)d0 + (off >> 4)) | (box >> 4) << 16, b_lo = a_lo + (a_boxes * box >> 4), hi = (uint32_t)(d0 >> 32);
+                for (uint32_t q = 0; q < steps; ++q)
+                    tc_mma_bf16_ss_elect(tmem + buf * 256, a_lo + q * 128, hi, b_lo + q * 128, hi, idesc, at > 0 || q > 0);
+                tc_commit_elect(smem_u32(&ctl->empty[rg.slot()]));
+                ++rg.n;
             }
             if (live) tc_commit_elect(smem_u32(&ctl->acc_full[buf]));
             ++it;
         }
-    } else if (warp >= 2) {
-        const int quarter = warp & 3, side = warp >= 6, row = quarter * 32 + lane;
+    } else {
+        // bf16 boxes of 128 rows x 64 columns in the layout of a swizzled TMA store, which cuts off what is behind the ends; as many
+        // units' worth of them as staging holds
+        const int quarter = warp & 3, side = warp >= 6, row = quarter * 32 + lane, tid = threadIdx.x - 64;
+        const int buffers = p.nb == 4 ? 1 : 2;
         int it = 0;
         for (Units w(p); w.more(); w.next()) {
             const int mt = w.mtile(), per = p.nb * 32, c0 = w.chunk() * p.nb * 64;
             const int rows = min(128, p.rows - mt * 128);
-            __nv_bfloat16* out = p.out + ((long long)w.e * p.rows + mt * 128) * p.cols + c0;
-            const bool some = w.n > 0;
-            bool ok = true;
-            if (some) {
-                const int buf = it & 1;
-                const uint32_t acc = tmem + buf * 256 + ((uint32_t)(quarter * 32) << 16);
-                ok = mbar_wait(smem_u32(&ctl->acc_full[buf]), (it >> 1) & 1, abort_flag, p.status);   // (given up: goes on without work)
-                tc_fence_after();
-                for (int c = 0; ok && c < per && quarter * 32 < rows && c0 + side * per + c < p.cols; c += 32) {
-                    float v[2][16];
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) tmem_ld16(acc + side * per + c + i * 16, v[i]);
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        tmem_ld_wait16(v[i]);
-                        stage_bf16(staging, 512, row, (side * per + c + i * 16) / 8, v[i]);
-                    }
-                }
-                tc_fence_before();
-                warp_arrive(smem_u32(&ctl->acc_empty[buf]), lane);
-                ++it;
-                epilogue_sync();
+            if (w.n == 0) {                                         // zeros: threads along rows, 16 bytes each
+                const int pieces = p.nb * 8, c = c0 + (tid & (pieces - 1)) * 8;
+                __nv_bfloat16* out = p.out + ((long long)w.e * p.rows + mt * 128) * p.cols + c;
+                if (c < p.cols)
+                    for (int r = tid / pieces; r < rows; r += 256 / pieces)
+                        *reinterpret_cast<uint4*>(out + (long long)r * p.cols) = make_uint4(0, 0, 0, 0);
+                continue;
             }
-            // threads along rows: as many pieces of 16 bytes as a unit is wide, a power of two
-            const int pieces = p.nb * 8, piece = (threadIdx.x - 64) & (pieces - 1), step = 256 / pieces;
-            if (ok && c0 + piece * 8 < p.cols)
-#pragma unroll 4
-                for (int r = (threadIdx.x - 64) / pieces; r < rows; r += step) {
-                    uint4 v = make_uint4(0, 0, 0, 0);
-                    if (some) v = ld_piece(staged(staging, 512, r, piece));
-                    *reinterpret_cast<uint4*>(out + (long long)r * p.cols + piece * 8) = v;
+            const int buf = it & 1;
+            const uint32_t acc = tmem + buf * 256 + ((uint32_t)(quarter * 32) << 16), to = staging + (it & (buffers - 1)) * (2 * 16384);
+            const bool ok = mbar_wait(smem_u32(&ctl->acc_full[buf]), (it >> 1) & 1, abort_flag, p.status);   // (given up: goes on without work)
+            tc_fence_after();
+            if (tid == 0) buffers == 2 ? bulk_read_done<1>() : bulk_read_done<0>();
+            epilogue_sync();
+            for (int c = 0; ok && c < per && quarter * 32 < rows && c0 + side * per + c < p.cols; c += 32) {
+                float v[2][16];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) tmem_ld16(acc + side * per + c + i * 16, v[i]);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    tmem_ld_wait16(v[i]);
+                    const int col = side * per + c + i * 16;
+                    st_piece(staged(to + col / 64 * 16384, 128, row, col % 64 / 8), pack8(v[i], 0));
+                    st_piece(staged(to + col / 64 * 16384, 128, row, col % 64 / 8 + 1), pack8(v[i], 8));
                 }
-            if (some) epilogue_sync();
+            }
+            tc_fence_before();
+            warp_arrive(smem_u32(&ctl->acc_empty[buf]), lane);
+            ++it;
+            fence_async_smem();
+            epilogue_sync();
+            if (tid == 0) {
+                for (int b = 0; ok && b < p.nb && c0 + b * 64 < p.cols; ++b) tma_store_3d(&mout, to + b * 16384, c0 + b * 64, mt * 128, w.e);
+                bulk_commit();
+            }
         }
+        if (tid == 0) bulk_all_done();
     }
     close_cta(ctl, tmem, warp);
 }
 
 // ------------------------------------------------------------------------------------------------ joining the slots
-// dX[t] = sum over the token's slots of their rows (fp16 behind a scale per 128 columns); dgate[p] = sum of its parts.  A pair
+// dX[t] = sum over the token's slots of their rows (fp16 behind a scale per 32 columns); dgate[p] = sum of its parts.  A pair
 // whose id is no expert was in no tile: it adds nothing and its gate gradient is 0.
 struct JoinParams {
     const int32_t* idx;
     const __half* dx;
-    const float* dx_scale;
+    const uint8_t* dx_scale;
     const float* dgate_part;
-    int P, T, k, h, M, dx_groups, parts, group_cols;
+    int P, T, k, h, M, dx_groups, parts;
     __nv_bfloat16* out_dx;
     float* out_dgate;
 };
@@ -755,12 +837,12 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ JoinP
     const long long all = p.out_dx ? (long long)p.T * vecs : 0;
     const long long first = (long long)blockIdx.x * 256 + threadIdx.x, stride = (long long)gridDim.x * 256;
     for (long long i = first; i < all; i += stride) {
-        const int t = (int)(i / vecs), c = (int)(i % vecs) * 8, grp = c / p.group_cols;
+        const int t = (int)(i / vecs), c = (int)(i % vecs) * 8;
         float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
         for (int j = 0; j < p.k; ++j) {
             const long long pair = (long long)t * p.k + j;
             if ((unsigned)p.idx[pair] >= (unsigned)p.M) continue;
-            const float sc = p.dx_scale[pair * p.dx_groups + grp];
+            const float sc = __int_as_float((int)p.dx_scale[pair * p.dx_groups + c / 32] << 23);
             const uint4 u = *reinterpret_cast<const uint4*>(p.dx + pair * p.h + c);
             const __half2* q = reinterpret_cast<const __half2*>(&u);
 #pragma unroll
@@ -797,7 +879,6 @@ struct Workspace {                 // offsets of the pieces, and the total
     size_t act = 0, du = 0, ga = 0, dgate = 0, dx = 0, dx_scale = 0, total = 0;
 };
 int back_boxes(int s) { return s > 192 ? 4 : (s + 63) / 64; }      // boxes of s rows per unit of the activation's backward
-int dx_group_cols(int h) { return h > 128 ? 128 : (h > 64 ? 64 : 32); }   // columns that share a scale: half a unit of kBackX
 int row_boxes(int h) { return h > 128 ? 4 : (h > 64 ? 2 : 1); }
 
 Workspace lay_out(int T, int h, int s, int M, int k, bool backward)
@@ -808,30 +889,30 @@ Workspace lay_out(int T, int h, int s, int M, int k, bool backward)
     if (!backward) {
         w.act = at; at += up256(P * s * 2);
     } else {
-        const int nb = back_boxes(s), chunks = (s + nb * 64 - 1) / (nb * 64), g = dx_group_cols(h);
+        const int nb = back_boxes(s), chunks = (s + nb * 64 - 1) / (nb * 64);
         w.du = at; at += up256(P * s * 4);
         w.ga = at; at += up256(P * s * 2);
         w.dgate = at; at += up256(P * 4 * chunks);
         w.dx = at; at += up256(P * h * 2);
-        w.dx_scale = at; at += up256(P * 4 * ((h + g - 1) / g));
+        w.dx_scale = at; at += up256(P * (((size_t)h + 31) / 32));
     }
     w.total = at;
     return w;
 }
 
-// 2-D [rows][cols]; for gathering loads the box is one row high.
+// 2-D [rows][cols], boxes of `high` rows x 64 columns; one row high for gathers.
 int rows_map(const void* ptr, long long rows, int cols, int high, CUtensorMap* out)
 {
     const uint64_t dims[2] = {(uint64_t)cols, (uint64_t)rows}, strides[1] = {(uint64_t)cols * 2};
     const uint32_t box[2] = {64, (uint32_t)high};
     return encode_tensor_map(ptr, 2, dims, strides, box, out);
 }
-// Weights [M][rows][cols], box 64 x 64 of one expert.
-int weight_map(const void* ptr, int M, int rows, int cols, CUtensorMap* out)
+// Weights [M][rows][cols], boxes of `high` rows x 64 columns of one expert.
+int weight_map(const void* ptr, int M, int rows, int cols, int high, CUtensorMap* out)
 {
     const uint64_t dims[3] = {(uint64_t)cols, (uint64_t)rows, (uint64_t)M};
     const uint64_t strides[2] = {(uint64_t)cols * 2, (uint64_t)rows * cols * 2};
-    const uint32_t box[3] = {64, 64, 1};
+    const uint32_t box[3] = {64, (uint32_t)high, 1};
     return encode_tensor_map(ptr, 3, dims, strides, box, out);
 }
 
@@ -845,12 +926,11 @@ template <int MODE>
 int launch_rows(const CUtensorMap& ma, const CUtensorMap& mw, RowsParams p, long long tiles, const DeviceCtx& ctx, cudaStream_t st)
 {
     if (allow_smem(rows_kernel<MODE>) != MORE_OK) return MORE_ERR_CUDA;
-    p.stages = kXRing / (kATile + p.nb * kBox);
-    if (p.stages > kXMaxStages) p.stages = kXMaxStages;
     p.status = ctx.status;
     const long long units = tiles * p.chunks;
+    if (units > 0x7fff0000LL) return MORE_ERR_TOO_LARGE;
     const int grid = units < ctx.sm_count ? (int)units : ctx.sm_count;
-    rows_kernel<MODE><<<grid, MODE == kUp || MODE == kBackAct ? kXGatherThreads : kXThreads, kXSmem, st>>>(ma, mw, p);
+    rows_kernel<MODE><<<grid, threads_of(MODE == kUp || MODE == kBackAct ? kLoaders : kFewLoaders), kXSmem, st>>>(ma, mw, p);
     count_launch(1);
     return cudaGetLastError() == cudaSuccess ? MORE_OK : MORE_ERR_CUDA;
 }
@@ -863,19 +943,20 @@ int launch_tiles(const ExpertsArgs& a, cudaStream_t st)
     return cudaGetLastError() == cudaSuccess ? MORE_OK : MORE_ERR_CUDA;
 }
 
-int launch_weights(const CUtensorMap& mtoken, const CUtensorMap& mplace, const CUtensorMap& mplace16, WeightsParams p, const DeviceCtx& ctx, cudaStream_t st)
+int launch_weights(const CUtensorMap& mtoken, const CUtensorMap (&mplace)[2], WeightsParams p, const DeviceCtx& ctx, cudaStream_t st)
 {
+    CUtensorMap mout;
+    const int rc = weight_map(p.out, p.M, p.rows, p.cols, 128, &mout);
+    if (rc != MORE_OK) return rc;
     if (allow_smem(weights_kernel) != MORE_OK) return MORE_ERR_CUDA;
     p.nb = p.cols > 128 ? 4 : (p.cols > 64 ? 2 : 1);
     p.mtiles = (p.rows + 127) / 128;
     p.chunks = (p.cols + p.nb * 64 - 1) / (p.nb * 64);
-    p.stages = kXRing / ((2 + p.nb) * kBox);
-    if (p.stages > kXMaxStages) p.stages = kXMaxStages;
     p.status = ctx.status;
     const long long units = (long long)p.M * p.mtiles * p.chunks;
-    if (units > 0x7fffffffLL) return MORE_ERR_TOO_LARGE;
+    if (units > 0x7fff0000LL) return MORE_ERR_TOO_LARGE;
     const int grid = units < ctx.sm_count ? (int)units : ctx.sm_count;
-    weights_kernel<<<grid, kXGatherThreads, kXSmem, st>>>(mtoken, mplace, mplace16, p);
+    weights_kernel<<<grid, threads_of(kLoaders), kXSmem, st>>>(mtoken, mplace[0], mplace[1], mout, p);
     count_launch(1);
     return cudaGetLastError() == cudaSuccess ? MORE_OK : MORE_ERR_CUDA;
 }
@@ -888,15 +969,16 @@ int launch_experts(const ExpertsArgs& a, const DeviceCtx& ctx)
     CUtensorMap mx, mact, m1, m2;
     int rc = rows_map(a.X, a.T, a.h, 1, &mx);
     if (rc == MORE_OK) rc = rows_map(base + w.act, P, a.s, 32, &mact);
-    if (rc == MORE_OK) rc = weight_map(a.W1, a.M, a.h, 2 * a.s, &m1);
-    if (rc == MORE_OK) rc = weight_map(a.W2, a.M, a.s, a.h, &m2);
+    if (rc == MORE_OK) rc = weight_map(a.W1, a.M, a.h, 2 * a.s, 64, &m1);
+    if (rc == MORE_OK) rc = weight_map(a.W2, a.M, a.s, a.h, 64, &m2);
     if (rc == MORE_OK) rc = launch_tiles(a, a.stream);
     if (rc != MORE_OK) return rc;
     RowsParams p{};
     p.tiles = static_cast<const int4*>(a.workspace);
     p.pairs = a.pairs;
-    p.P = (int)P; p.k = a.k; p.h = a.h; p.s = a.s;
+    p.P = (int)P; p.h = a.h; p.s = a.s;
     const long long tiles = tile_capacity(a.T, a.M, a.k);
+    p.by_k.by(a.k);
     p.rows = a.T;
     p.nb = a.s > 64 ? 4 : 2;
     p.chunks = (a.s + p.nb * 32 - 1) / (p.nb * 32);
@@ -905,7 +987,6 @@ int launch_experts(const ExpertsArgs& a, const DeviceCtx& ctx)
     p.hidden = a.out_hidden;
     rc = launch_rows<kUp>(mx, m1, p, tiles, ctx, a.stream);
     if (rc != MORE_OK) return rc;
-    p.rows = (int)P;
     p.nb = row_boxes(a.h);
     p.chunks = (a.h + p.nb * 64 - 1) / (p.nb * 64);
     p.ksteps = (a.s + 63) / 64;
@@ -918,20 +999,22 @@ int launch_experts_backward(const ExpertsArgs& a, const DeviceCtx& ctx)
     const long long P = (long long)a.T * a.k;
     const Workspace w = lay_out(a.T, a.h, a.s, a.M, a.k, true);
     char* base = static_cast<char*>(a.workspace);
-    CUtensorMap mx, md, mdu[3], mga[2], m1, m2;             // by token; by place one row, 16 rows and 32 rows high; weights
+    CUtensorMap mx, md, mdu[2], mdu32, mga[2], m1, m2;             // rows by token; by place one row, 16 and 32 rows high; weights
     int rc = rows_map(a.X, a.T, a.h, 1, &mx);
     if (rc == MORE_OK) rc = rows_map(a.dout, a.T, a.h, 1, &md);
-    for (int i = 0; i < 3 && rc == MORE_OK; ++i) rc = rows_map(base + w.du, P, 2 * a.s, i == 0 ? 1 : 8 << i, &mdu[i]);
+    for (int i = 0; i < 2 && rc == MORE_OK; ++i) rc = rows_map(base + w.du, P, 2 * a.s, i == 0 ? 1 : 16, &mdu[i]);
+    if (rc == MORE_OK) rc = rows_map(base + w.du, P, 2 * a.s, 32, &mdu32);
     for (int i = 0; i < 2 && rc == MORE_OK; ++i) rc = rows_map(base + w.ga, P, a.s, i == 0 ? 1 : 16, &mga[i]);
-    if (rc == MORE_OK) rc = weight_map(a.W1, a.M, a.h, 2 * a.s, &m1);
-    if (rc == MORE_OK) rc = weight_map(a.W2, a.M, a.s, a.h, &m2);
+    if (rc == MORE_OK) rc = weight_map(a.W1, a.M, a.h, 2 * a.s, row_boxes(a.h) * 64, &m1);
+    if (rc == MORE_OK) rc = weight_map(a.W2, a.M, a.s, a.h, back_boxes(a.s) * 64, &m2);
     if (rc == MORE_OK) rc = launch_tiles(a, a.stream);
     if (rc != MORE_OK) return rc;
     const long long tiles = tile_capacity(a.T, a.M, a.k);
     RowsParams p{};
     p.tiles = static_cast<const int4*>(a.workspace);
     p.pairs = a.pairs;
-    p.P = (int)P; p.k = a.k; p.h = a.h; p.s = a.s;
+    p.P = (int)P; p.h = a.h; p.s = a.s;
+    p.by_k.by(a.k);
     p.rows = a.T;
     p.nb = back_boxes(a.s);
     p.chunks = (a.s + p.nb * 64 - 1) / (p.nb * 64);
@@ -944,22 +1027,20 @@ int launch_experts_backward(const ExpertsArgs& a, const DeviceCtx& ctx)
     const int parts = p.chunks;
     rc = launch_rows<kBackAct>(md, m2, p, tiles, ctx, a.stream);
     if (rc != MORE_OK) return rc;
-    p.dx_groups = (a.h + dx_group_cols(a.h) - 1) / dx_group_cols(a.h);
+    p.dx_groups = (a.h + 31) / 32;
     p.dx = reinterpret_cast<__half*>(base + w.dx);
-    p.dx_scale = reinterpret_cast<float*>(base + w.dx_scale);
+    p.dx_scale = reinterpret_cast<uint8_t*>(base + w.dx_scale);
     if (a.out_dx) {
-        p.rows = (int)P;
         p.nb = row_boxes(a.h);
         p.chunks = (a.h + p.nb * 64 - 1) / (p.nb * 64);
         p.ksteps = (2 * a.s + 63) / 64;
-        rc = launch_rows<kBackX>(mdu[2], m1, p, tiles, ctx, a.stream);
+        rc = launch_rows<kBackX>(mdu32, m1, p, tiles, ctx, a.stream);
         if (rc != MORE_OK) return rc;
     }
     if (a.out_dx || a.out_dgate) {
         JoinParams j{};
         j.idx = a.idx; j.dx = p.dx; j.dx_scale = p.dx_scale; j.dgate_part = p.dgate_part;
         j.P = (int)P; j.T = a.T; j.k = a.k; j.h = a.h; j.M = a.M; j.dx_groups = p.dx_groups; j.parts = parts;
-        j.group_cols = dx_group_cols(a.h);
         j.out_dx = a.out_dx; j.out_dgate = a.out_dgate;
         const long long items = a.out_dx ? (long long)a.T * (a.h / 8) : P;
         const long long blocks = (items + 255) / 256;
@@ -968,15 +1049,17 @@ int launch_experts_backward(const ExpertsArgs& a, const DeviceCtx& ctx)
         if (cudaGetLastError() != cudaSuccess) return MORE_ERR_CUDA;
     }
     WeightsParams q{};
-    q.offsets = a.offsets; q.pairs = a.pairs; q.P = (int)P; q.T = a.T; q.k = a.k; q.M = a.M;
+    q.offsets = a.offsets; q.pairs = a.pairs; q.P = (int)P; q.T = a.T; q.by_k.by(a.k); q.M = a.M;
     if (a.out_dw1) {
-        q.a_by_token = 1; q.rows = a.h; q.cols = 2 * a.s; q.out = a.out_dw1;
-        rc = launch_weights(mx, mdu[0], mdu[1], q, ctx, a.stream);
+        q.a_by_token = 1;
+        q.rows = a.h; q.cols = 2 * a.s; q.out = a.out_dw1;
+        rc = launch_weights(mx, mdu, q, ctx, a.stream);
         if (rc != MORE_OK) return rc;
     }
     if (a.out_dw2) {
-        q.a_by_token = 0; q.rows = a.s; q.cols = a.h; q.out = a.out_dw2;
-        rc = launch_weights(md, mga[0], mga[1], q, ctx, a.stream);
+        q.a_by_token = 0;
+        q.rows = a.s; q.cols = a.h; q.out = a.out_dw2;
+        rc = launch_weights(md, mga, q, ctx, a.stream);
     }
     return rc;
 }
