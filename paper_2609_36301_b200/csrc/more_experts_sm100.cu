@@ -199,6 +199,9 @@ __global__ void __launch_bounds__(1024) tiles_kernel(const int32_t* __restrict__
 
 // Barrier of the eight epilogue warps.
 __device__ __forceinline__ void epilogue_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
+// Four of them hand two buffers to the other four and back: barriers 2, 3: a buffer is full; 4, 5: it is free again.
+__device__ __forceinline__ void hand_over(int barrier) { asm volatile("bar.arrive %0, 256;" ::"r"(barrier) : "memory"); }
+__device__ __forceinline__ void take_over(int barrier) { asm volatile("bar.sync %0, 256;" ::"r"(barrier) : "memory"); }
 
 __device__ __forceinline__ void st_piece(uint32_t at, uint4 v)
 {
@@ -238,8 +241,8 @@ __device__ __forceinline__ uint4 pack8_half(const float (&v)[16], int at, float 
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// Common start of both kernels: barriers, tensor memory.  Returns the tensor-memory base.
-__device__ __forceinline__ uint32_t open_cta(Control* c, int warp)
+// Common start of both kernels: barriers, tensor memory.  readers: warps that read an accumulator.  Returns the tensor-memory base.
+__device__ __forceinline__ uint32_t open_cta(Control* c, int readers, int warp)
 {
     if (threadIdx.x == 0) {
         for (int i = 0; i < kSlots; ++i) {
@@ -248,7 +251,7 @@ __device__ __forceinline__ uint32_t open_cta(Control* c, int warp)
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(smem_u32(&c->acc_full[i]), 1);
-            mbar_init(smem_u32(&c->acc_empty[i]), 8);
+            mbar_init(smem_u32(&c->acc_empty[i]), readers);
         }
         c->abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -382,12 +385,13 @@ rows_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUte
 {
     constexpr bool kGather = MODE == kUp || MODE == kBackAct;       // rows of A are tokens', else places in expert order
     constexpr bool kMn = MODE == kUp || MODE == kDown;              // weights as an MN-major operand
+    constexpr bool kCompute = kGather;                              // values are worked on behind the product, not only rounded
     extern __shared__ uint8_t smem_raw[];
     const uint32_t ring = (smem_u32(smem_raw) + 1023u) & ~1023u, staging = ring + kXRing;
     uint8_t* const staging_at = smem_raw + (ring - smem_u32(smem_raw)) + kXRing;
     Control* ctl = reinterpret_cast<Control*>(staging_at + kXStaging);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t tmem = open_cta(ctl, warp);
+    const uint32_t tmem = open_cta(ctl, kCompute ? 8 : 4, warp);
     volatile int* abort_flag = &ctl->abort;
     const int units = p.tiles[0].x * p.chunks;
 
@@ -457,16 +461,14 @@ rows_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUte
             }
             if (live) tc_commit_elect(smem_u32(&ctl->acc_full[buf]));
         }
-    } else {
-        // The accumulator comes thread by row; memory is written along rows, so values pass through staging.  Where there is work to
-        // be done on them (kUp, kBackAct) all eight warps do it along rows, so that a tile of few rows occupies them all; where
-        // they are only rounded, each warp handles its own rows and columns and waits for nobody.
+    } else if constexpr (kCompute) {
+        // Two steps per pass: the warps that have rows copy columns of the accumulator into staging, thread by row; then all
+        // eight work along rows, so that memory is read and written in whole lines and a tile of few rows occupies them all.
         const int quarter = warp & 3, side = warp >= 6;             // lane quarter of the accumulator; half of the columns
         const int r0 = quarter * 32, row = r0 + lane;               // this warp's first row of a tile, this thread's
         const int tid = threadIdx.x - 64;
         int it = 0;
-        // (pairs: of row `row` in kBackAct, of row `tid` in the others' warps of the first half)
-        for (TilesAhead<MODE == kUp ? 0 : 1> u(p, units, MODE == kBackAct ? row : tid & 127); u.more(); u.next(), ++it) {
+        for (TilesAhead<MODE == kUp ? 0 : 1> u(p, units, row); u.more(); u.next(), ++it) {
             const int4 tile = u.tile;
             const int chunk = u.chunk, buf = it & 1;
             const uint32_t acc = tmem + buf * 256 + ((uint32_t)r0 << 16);
@@ -523,7 +525,7 @@ rows_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUte
                     }
                     epilogue_sync();
                 }
-            } else if constexpr (MODE == kBackAct) {
+            } else {
                 const int width = p.nb * 64, passes = (min(width, p.s - chunk * width) + 63) / 64;
                 if (side == 0) ctl->pair[row] = u.pair[0];          // (the last tile's have been read)
                 float dg[4] = {0.f, 0.f, 0.f, 0.f};
@@ -578,17 +580,33 @@ rows_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUte
                     if ((tid & 7) == 0 && pair >= 0) p.dgate_part[(long long)chunk * p.P + pair] = dg[i];
                 }
                 epilogue_sync();
-            } else {
-                const int per = p.nb * 32, c0 = chunk * p.nb * 64;
-                const int unlike = unlike_boxes(tile.z), copy = quarter / unlike, mine = (quarter % unlike) * 32 + lane;
-                if (side == 0) ctl->pair[tid] = u.pair[0];          // (the last unit's have been read)
-                if ((quarter % unlike) * 32 < rows)
-                    for (int c = copy * 32; c < per && c0 + side * per + c < p.h; c += 4 / unlike * 32) {
+            }
+        }
+    } else if (warp < 6) {
+        // The accumulator comes thread by row, memory is written along rows: these four warps round it into one of two buffers of 64
+        // rows, the next four write buffers out.  (An SM writes about 25 bytes a clock; where the same warps did both, that time
+        // came on top of the rest.)
+        const int quarter = warp & 3, tid = threadIdx.x - 64;       // lane quarter of the accumulator
+        int it = 0, piece = 0;
+        for (TilesAhead<1> u(p, units, tid); u.more(); u.next(), ++it) {
+            const int buf = it & 1, c0 = u.chunk * p.nb * 64, cols = min(p.nb * 64, p.h - c0);
+            const uint32_t acc = tmem + buf * 256 + ((uint32_t)(quarter * 32) << 16);
+            // (after a wait that gave up the loop goes on without work: no warp is left alone at a barrier)
+            const bool ok = mbar_wait(smem_u32(&ctl->acc_full[buf]), (it >> 1) & 1, abort_flag, p.status);
+            tc_fence_after();
+            const int unlike = unlike_boxes(u.tile.z), copy = quarter / unlike, pieces = u.tile.z > 64 ? 2 : 1;
+            for (int q = 0; q < pieces; ++q, ++piece) {
+                const int b = piece & 1, first = (quarter % unlike) * 32 - q * 64;        // this warp's first row in the buffer
+                if (piece >= 2) take_over(4 + b);
+                if (tid >> 6 == q) ctl->pair[b * 64 + (tid & 63)] = ok ? u.pair[0] : -1;
+                if (ok && first >= 0 && first < 64 && q * 64 + first < u.tile.z)
+                    for (int c = copy * 32; c < cols; c += 4 / unlike * 32) {
                         float v[2][16];
-                        tmem_ld16(acc + side * per + c, v[0]);
-                        tmem_ld16(acc + side * per + c + 16, v[1]);
+                        tmem_ld16(acc + c, v[0]);
+                        tmem_ld16(acc + c + 16, v[1]);
                         tmem_ld_wait16(v[0]); tmem_ld_wait16(v[1]);
-                        const uint32_t to = staging + mine * kRowPitch + (side * per + c) * 2;
+                        const int at = (b * 64 + first + lane) * kRowPitch;
+                        const uint32_t to = staging + at + c * 2;
                         if constexpr (MODE == kDown) {
                             st_piece(to, pack8(v[0], 0)); st_piece(to + 16, pack8(v[0], 8));
                             st_piece(to + 32, pack8(v[1], 0)); st_piece(to + 48, pack8(v[1], 8));
@@ -603,24 +621,38 @@ rows_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUte
                             const float up = ex < 255 ? __int_as_float((268 - ex) << 23) : 1.f;
                             st_piece(to, pack8_half(v[0], 0, up)); st_piece(to + 16, pack8_half(v[0], 8, up));
                             st_piece(to + 32, pack8_half(v[1], 0, up)); st_piece(to + 48, pack8_half(v[1], 8, up));
-                            staging_at[mine * kRowPitch + 512 + (side * per + c) / 32] = (uint8_t)(ex < 255 ? ex - 14 : 127);   // (behind the row)
+                            staging_at[at + 512 + c / 32] = (uint8_t)(ex < 255 ? ex - 14 : 127);   // (behind the row)
                         }
                     }
-                release();
-                epilogue_sync();
-                // a warp per row: up to 512 consecutive bytes
-                uint16_t* out = MODE == kDown ? reinterpret_cast<uint16_t*>(p.out) : reinterpret_cast<uint16_t*>(p.dx);
-                const bool in = lane < p.nb * 8 && c0 + lane * 8 < p.h;
-                for (int r = warp - 2; r < rows; r += 32) {
+                if (q == pieces - 1) {
+                    tc_fence_before();
+                    warp_arrive(smem_u32(&ctl->acc_empty[buf]), lane);
+                }
+                hand_over(2 + b);
+            }
+        }
+        if (piece >= 2) take_over(4 + (piece & 1));                  // (every hand-over is taken)
+        if (piece >= 1) take_over(4 + ((piece - 1) & 1));
+    } else {
+        // a warp per row: up to 512 consecutive bytes
+        int piece = 0;
+        uint16_t* out = MODE == kDown ? reinterpret_cast<uint16_t*>(p.out) : reinterpret_cast<uint16_t*>(p.dx);
+        for (TilesAhead<0> u(p, units, 0); u.more(); u.next()) {
+            const int c0 = u.chunk * p.nb * 64, pieces = u.tile.z > 64 ? 2 : 1;
+            const bool in = lane < p.nb * 8 && c0 + lane * 8 < p.h;
+            for (int q = 0; q < pieces; ++q, ++piece) {
+                const int b = piece & 1, rows = min(64, u.tile.z - q * 64);
+                take_over(2 + b);
+                for (int r = warp - 6; r < rows; r += 16) {
                     uint4 v[4];
                     int pair[4];
                     uint8_t ex[4];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const int q = min(r + 8 * i, kTileRows - 1);
-                        pair[i] = r + 8 * i < rows ? ctl->pair[q] : -1;
-                        v[i] = ld_piece(staging_at + q * kRowPitch + lane * 16);
-                        if (MODE == kBackX) ex[i] = staging_at[q * kRowPitch + 512 + (lane & 7)];
+                        const int at = b * 64 + min(r + 4 * i, 63);
+                        pair[i] = r + 4 * i < rows ? ctl->pair[at] : -1;
+                        v[i] = ld_piece(staging_at + at * kRowPitch + lane * 16);
+                        if (MODE == kBackX) ex[i] = staging_at[at * kRowPitch + 512 + (lane & 7)];
                     }
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
@@ -629,7 +661,7 @@ rows_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUte
                         if (MODE == kBackX && lane < p.nb * 2 && c0 + lane * 32 < p.h) p.dx_scale[(long long)pair[i] * p.dx_groups + c0 / 32 + lane] = ex[i];
                     }
                 }
-                epilogue_sync();
+                hand_over(4 + b);
             }
         }
     }
@@ -693,7 +725,7 @@ weights_kernel(const __grid_constant__ CUtensorMap mtoken, const __grid_constant
     uint8_t* const staging_at = smem_raw + (ring - smem_u32(smem_raw)) + kXRing;
     Control* ctl = reinterpret_cast<Control*>(staging_at + kXStaging);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t tmem = open_cta(ctl, warp);
+    const uint32_t tmem = open_cta(ctl, 8, warp);
     volatile int* abort_flag = &ctl->abort;
 
     if (warp == 0 || warp >= 10) {
