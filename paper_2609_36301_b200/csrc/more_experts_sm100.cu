@@ -209,8 +209,27 @@ __device__ __forceinline__ void st_piece(uint32_t at, uint4 v)
 }
 // (Not volatile: several may be in flight.  The barriers around them keep them in their place.)
 __device__ __forceinline__ uint4 ld_piece(const uint8_t* at) { return *reinterpret_cast<const uint4*>(at); }
-// fp32 staging: rows of `pitch` bytes, a power of two; the 16-byte pieces of a row are permuted by the row's number, so that neither
-// a warp that writes a piece of 32 rows nor one that reads along a row meets itself on a bank.
+// Rows of staging (of kPrivatePitch bytes, written by this warp's threads) to memory, 16 bytes a thread, `pieces` (4 or 8) a row; dst: of
+// row 0, ld: from row to row; limit: columns to write.
+constexpr int kPrivatePitch = 144;                   // 64 16-bit values, and 16 bytes so that rows fall on other banks
+static_assert(8 * 32 * kPrivatePitch <= kXStaging, "staging");
+__device__ __forceinline__ void write_rows(const uint8_t* from, int pieces, int lane, int rows, int limit, __nv_bfloat16* dst, int ld)
+{
+    __syncwarp();
+    const int piece = lane & (pieces - 1), first = lane / pieces, step = 32 / pieces;
+    const bool in = piece * 8 < limit;
+    for (int r = first; r - first < rows; r += 4 * step) {          // (four loads, then four stores)
+        uint4 v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = ld_piece(from + ((r + i * step) & 31) * kPrivatePitch + piece * 16);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (in && r + i * step < rows) *reinterpret_cast<uint4*>(dst + (long long)(r + i * step) * ld + piece * 8) = v[i];
+    }
+    __syncwarp();
+}
+// Rows of `pitch` bytes, a power of two; the 16-byte pieces of a row are permuted by the row's number, so that neither a warp that
+// writes a piece of 32 rows nor one that reads along a row meets itself on a bank (pitch 128: the layout of a TMA box).
 __device__ __forceinline__ uint32_t staged(uint32_t base, int pitch, int row, int piece) { return base + row * pitch + ((piece ^ (row & 7)) << 4); }
 __device__ __forceinline__ void stage_f32(uint32_t base, int pitch, int row, int piece, const float (&v)[16])
 {
@@ -461,27 +480,67 @@ rows_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUte
             }
             if (live) tc_commit_elect(smem_u32(&ctl->acc_full[buf]));
         }
-    } else if constexpr (kCompute) {
+    } else if constexpr (MODE == kUp) {
+        // Thread by row: a warp works on 32 rows and half of the columns, and passes what it has to write through staging of its own, so
+        // that it is written along rows.
+        const int quarter = warp & 3, side = warp >= 6;             // lane quarter of the accumulator; half of the columns
+        const int r0 = quarter * 32;                                // this warp's first row of a tile
+        const uint32_t at = (warp - 2) * 32 * kPrivatePitch;        // of this warp's staging
+        const uint32_t mine = staging + at + lane * kPrivatePitch;
+        int it = 0;
+        for (TilesAhead<0> u(p, units, 0); u.more(); u.next(), ++it) {
+            const int buf = it & 1, rows = min(32, u.tile.z - r0), place0 = u.tile.y + r0;
+            const uint32_t acc = tmem + buf * 256 + ((uint32_t)r0 << 16);
+            const int cols = p.nb * 32, per = cols / 2, s0 = u.chunk * cols + side * per;      // s columns of the unit; of this warp
+            if (!mbar_wait(smem_u32(&ctl->acc_full[buf]), (it >> 1) & 1, abort_flag, p.status)) break;
+            tc_fence_after();
+            if (rows > 0 && s0 < p.s) {
+                const int limit = min(per, p.s - s0);
+                if (p.hidden)
+                    for (int half = 0; half < 2; ++half) {
+                        for (int c = 0; c < limit; c += 16) {
+                            float v[16];
+                            tmem_ld16(acc + half * cols + side * per + c, v);
+                            tmem_ld_wait16(v);
+                            st_piece(mine + c * 2, pack8(v, 0));
+                            st_piece(mine + c * 2 + 16, pack8(v, 8));
+                        }
+                        write_rows(staging_at + at, per / 8, lane, rows, limit, p.hidden + (long long)place0 * 2 * p.s + half * p.s + s0, 2 * p.s);
+                    }
+                for (int c = 0; c < limit; c += 16) {
+                    float g[16], v[16];
+                    tmem_ld16(acc + side * per + c, g);
+                    tmem_ld16(acc + cols + side * per + c, v);
+                    tmem_ld_wait16(g); tmem_ld_wait16(v);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) g[i] = g[i] * sigmoidf(g[i]) * v[i];
+                    st_piece(mine + c * 2, pack8(g, 0));
+                    st_piece(mine + c * 2 + 16, pack8(g, 8));
+                }
+                write_rows(staging_at + at, per / 8, lane, rows, limit, p.out + (long long)place0 * p.s + s0, p.s);
+            }
+            tc_fence_before();
+            warp_arrive(smem_u32(&ctl->acc_empty[buf]), lane);
+        }
+    } else if constexpr (MODE == kBackAct) {
         // Two steps per pass: the warps that have rows copy columns of the accumulator into staging, thread by row; then all
         // eight work along rows, so that memory is read and written in whole lines and a tile of few rows occupies them all.
         const int quarter = warp & 3, side = warp >= 6;             // lane quarter of the accumulator; half of the columns
         const int r0 = quarter * 32, row = r0 + lane;               // this warp's first row of a tile, this thread's
         const int tid = threadIdx.x - 64;
         int it = 0;
-        for (TilesAhead<MODE == kUp ? 0 : 1> u(p, units, row); u.more(); u.next(), ++it) {
+        for (TilesAhead<1> u(p, units, row); u.more(); u.next(), ++it) {
             const int4 tile = u.tile;
             const int chunk = u.chunk, buf = it & 1;
             const uint32_t acc = tmem + buf * 256 + ((uint32_t)r0 << 16);
-            uint4 kept[4][2];                                       // kBackAct: both projections of this thread's first items
-            if constexpr (MODE == kBackAct) {
+            uint4 kept[4][2];                                       // both projections of this thread's first items
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int r = (i * 256 + tid) >> 3, col = chunk * p.nb * 64 + (tid & 7) * 8;
-                    if (r < tile.z && col < p.s) {
-                        const __nv_bfloat16* from = p.hidden + (long long)(tile.y + r) * 2 * p.s + col;
-                        kept[i][0] = *reinterpret_cast<const uint4*>(from);
-                        kept[i][1] = *reinterpret_cast<const uint4*>(from + p.s);
-                    }
+            for (int i = 0; i < 4; ++i) {
+                const int r = (i * 256 + tid) >> 3, col = chunk * p.nb * 64 + (tid & 7) * 8;
+                if (r < tile.z && col < p.s) {
+                    const __nv_bfloat16* from = p.hidden + (long long)(tile.y + r) * 2 * p.s + col;
+                    kept[i][0] = *reinterpret_cast<const uint4*>(from);
+                    kept[i][1] = *reinterpret_cast<const uint4*>(from + p.s);
                 }
             }
             // after a wait that gave up the loop goes on without work: no warp is left alone at a barrier
@@ -493,94 +552,60 @@ rows_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUte
                 tc_fence_before();
                 warp_arrive(smem_u32(&ctl->acc_empty[buf]), lane);
             };
-            if constexpr (MODE == kUp) {
-                const int cols = p.nb * 32, passes = (min(cols, p.s - chunk * cols) + 63) / 64;
-                for (int pass = 0; pass < passes; ++pass) {
-                    if (any) {                                      // 64 gate columns, then the 64 others: one half of each per warp
-                        float v[4][16];
+            const int width = p.nb * 64, passes = (min(width, p.s - chunk * width) + 63) / 64;
+            if (side == 0) ctl->pair[row] = u.pair[0];          // (the last tile's have been read)
+            float dg[4] = {0.f, 0.f, 0.f, 0.f};
+            for (int pass = 0; pass < passes; ++pass) {
+                if (any) {
+                    float v[2][16];
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) tmem_ld16(acc + (i >= 2 ? cols : 0) + pass * 64 + side * 32 + (i & 1) * 16, v[i]);
+                    for (int i = 0; i < 2; ++i) tmem_ld16(acc + pass * 64 + side * 32 + i * 16, v[i]);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            tmem_ld_wait16(v[i]);
-                            stage_f32(staging, 512, row, (i >= 2 ? 16 : 0) + side * 8 + (i & 1) * 4, v[i]);
-                        }
+                    for (int i = 0; i < 2; ++i) {
+                        tmem_ld_wait16(v[i]);
+                        stage_f32(staging, 256, row, side * 8 + i * 4, v[i]);
                     }
-                    if (pass == passes - 1) release();
-                    epilogue_sync();
-                    const int s0 = chunk * cols + pass * 64 + (tid & 7) * 8;
-                    for (int r = tid >> 3; r < rows; r += 32) {
-                        if (s0 >= p.s) continue;
-                        float g[8], w[8], a[8];
-                        unstage8(staging_at, 512, r, (tid & 7) * 2, g);
-                        unstage8(staging_at, 512, r, 16 + (tid & 7) * 2, w);
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) a[i] = g[i] * sigmoidf(g[i]) * w[i];
-                        const long long place = tile.y + r;
-                        *reinterpret_cast<uint4*>(p.out + place * p.s + s0) = pack8(a);
-                        if (p.hidden) {
-                            *reinterpret_cast<uint4*>(p.hidden + place * 2 * p.s + s0) = pack8(g);
-                            *reinterpret_cast<uint4*>(p.hidden + place * 2 * p.s + p.s + s0) = pack8(w);
-                        }
-                    }
-                    epilogue_sync();
                 }
-            } else {
-                const int width = p.nb * 64, passes = (min(width, p.s - chunk * width) + 63) / 64;
-                if (side == 0) ctl->pair[row] = u.pair[0];          // (the last tile's have been read)
-                float dg[4] = {0.f, 0.f, 0.f, 0.f};
-                for (int pass = 0; pass < passes; ++pass) {
-                    if (any) {
-                        float v[2][16];
-#pragma unroll
-                        for (int i = 0; i < 2; ++i) tmem_ld16(acc + pass * 64 + side * 32 + i * 16, v[i]);
-#pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            tmem_ld_wait16(v[i]);
-                            stage_f32(staging, 256, row, side * 8 + i * 4, v[i]);
-                        }
-                    }
-                    if (pass == passes - 1) release();
-                    epilogue_sync();
-                    const int s0 = chunk * width + pass * 64 + (tid & 7) * 8;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int r = (i * 256 + tid) >> 3;
-                        if (r >= rows || s0 >= p.s) continue;
-                        const long long place = tile.y + r;
-                        const __nv_bfloat16* from = p.hidden + place * 2 * p.s + s0;
-                        const uint4 hg = pass == 0 ? kept[i][0] : *reinterpret_cast<const uint4*>(from);
-                        const uint4 hu = pass == 0 ? kept[i][1] : *reinterpret_cast<const uint4*>(from + p.s);
-                        const int pair = ctl->pair[r];
-                        const float gate = pair >= 0 ? p.gate[pair] : 0.f;
-                        const uint32_t wg[4] = {hg.x, hg.y, hg.z, hg.w}, wu[4] = {hu.x, hu.y, hu.z, hu.w};
-                        float c[8], out_g[8], out_u[8], out_a[8];
-                        unstage8(staging_at, 256, r, (tid & 7) * 2, c);
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            const float g = j & 1 ? bf16_hi(wg[j / 2]) : bf16_lo(wg[j / 2]), up = j & 1 ? bf16_hi(wu[j / 2]) : bf16_lo(wu[j / 2]);
-                            const float sg = sigmoidf(g), silu = g * sg, act = silu * up, da = gate * c[j];
-                            dg[i] = fmaf(c[j], act, dg[i]);
-                            out_a[j] = gate * act;
-                            out_u[j] = da * silu;
-                            out_g[j] = da * up * fmaf(silu, 1.f - sg, sg);
-                        }
-                        *reinterpret_cast<uint4*>(p.du + place * 2 * p.s + s0) = pack8(out_g);
-                        *reinterpret_cast<uint4*>(p.du + place * 2 * p.s + p.s + s0) = pack8(out_u);
-                        if (p.ga) *reinterpret_cast<uint4*>(p.ga + place * p.s + s0) = pack8(out_a);
-                    }
-                    if (pass < passes - 1) epilogue_sync();
-                }
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {                       // the eight threads of a row
-                    const int r = (i * 256 + tid) >> 3;
-#pragma unroll
-                    for (int o = 4; o > 0; o >>= 1) dg[i] += __shfl_xor_sync(0xffffffffu, dg[i], o);
-                    const int pair = r < rows ? ctl->pair[r] : -1;
-                    if ((tid & 7) == 0 && pair >= 0) p.dgate_part[(long long)chunk * p.P + pair] = dg[i];
-                }
+                if (pass == passes - 1) release();
                 epilogue_sync();
+                const int s0 = chunk * width + pass * 64 + (tid & 7) * 8;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int r = (i * 256 + tid) >> 3;
+                    if (r >= rows || s0 >= p.s) continue;
+                    const long long place = tile.y + r;
+                    const __nv_bfloat16* from = p.hidden + place * 2 * p.s + s0;
+                    const uint4 hg = pass == 0 ? kept[i][0] : *reinterpret_cast<const uint4*>(from);
+                    const uint4 hu = pass == 0 ? kept[i][1] : *reinterpret_cast<const uint4*>(from + p.s);
+                    const int pair = ctl->pair[r];
+                    const float gate = pair >= 0 ? p.gate[pair] : 0.f;
+                    const uint32_t wg[4] = {hg.x, hg.y, hg.z, hg.w}, wu[4] = {hu.x, hu.y, hu.z, hu.w};
+                    float c[8], out_g[8], out_u[8], out_a[8];
+                    unstage8(staging_at, 256, r, (tid & 7) * 2, c);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const float g = j & 1 ? bf16_hi(wg[j / 2]) : bf16_lo(wg[j / 2]), up = j & 1 ? bf16_hi(wu[j / 2]) : bf16_lo(wu[j / 2]);
+                        const float sg = sigmoidf(g), silu = g * sg, act = silu * up, da = gate * c[j];
+                        dg[i] = fmaf(c[j], act, dg[i]);
+                        out_a[j] = gate * act;
+                        out_u[j] = da * silu;
+                        out_g[j] = da * up * fmaf(silu, 1.f - sg, sg);
+                    }
+                    *reinterpret_cast<uint4*>(p.du + place * 2 * p.s + s0) = pack8(out_g);
+                    *reinterpret_cast<uint4*>(p.du + place * 2 * p.s + p.s + s0) = pack8(out_u);
+                    if (p.ga) *reinterpret_cast<uint4*>(p.ga + place * p.s + s0) = pack8(out_a);
+                }
+                if (pass < passes - 1) epilogue_sync();
             }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {                       // the eight threads of a row
+                const int r = (i * 256 + tid) >> 3;
+#pragma unroll
+                for (int o = 4; o > 0; o >>= 1) dg[i] += __shfl_xor_sync(0xffffffffu, dg[i], o);
+                const int pair = r < rows ? ctl->pair[r] : -1;
+                if ((tid & 7) == 0 && pair >= 0) p.dgate_part[(long long)chunk * p.P + pair] = dg[i];
+            }
+            epilogue_sync();
         }
     } else if (warp < 6) {
         // The accumulator comes thread by row, memory is written along rows: these four warps round it into one of two buffers of 64
@@ -742,6 +767,7 @@ weights_kernel(const __grid_constant__ CUtensorMap mtoken, const __grid_constant
                 const int left = min(64, u.n - at), steps = (left + 15) / 16;
                 const uint32_t box = (uint32_t)steps * 2048;
                 uint32_t where;
+                const uint32_t bytes = box * (a_boxes + p.nb);
                 if (rg.n % kLoaders == loader) {
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
@@ -752,9 +778,9 @@ weights_kernel(const __grid_constant__ CUtensorMap mtoken, const __grid_constant
                     }
                     __syncwarp();
                 }
-                if (!rg.open(box * (a_boxes + p.nb), loader, kLoaders, ctl, lane, abort_flag, p.status, &where, &live)) continue;
+                if (!rg.open(bytes, loader, kLoaders, ctl, lane, abort_flag, p.status, &where, &live)) continue;
                 const uint32_t full = smem_u32(&ctl->full[rg.slot()]);
-                expect_elect(full, box * (a_boxes + p.nb));
+                expect_elect(full, bytes);
                 const uint32_t a_at = ring + where, b_at = a_at + a_boxes * box;
                 const int a_x = mt * 128, b_x = chunk * p.nb * 64;
                 const int t_boxes = p.a_by_token ? a_boxes : p.nb, p_boxes = p.a_by_token ? p.nb : a_boxes;
