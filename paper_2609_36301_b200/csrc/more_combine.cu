@@ -10,8 +10,9 @@
 // Bound by the bytes of the rows.  A token's row is spread over a warp (up to 1024 columns) or over a CTA, eight columns per
 // 16-byte load, and stays in registers between the two sums of squares, so that everything is read once and written once.  All
 // sums are 32-bit; rows are rounded where they are written.  The backward's column sums stay in registers while a CTA goes
-// through its tokens; a second kernel adds the CTAs' parts in order, so that results do not depend on timing.
-#include "more_internal.h"
+// through its tokens, whose rows come through a ring in shared memory; a second kernel adds the CTAs' parts in order, so that
+// results do not depend on timing.
+#include "sm100_common.cuh"
 
 namespace more {
 
@@ -19,7 +20,14 @@ namespace {
 
 constexpr unsigned kAll = 0xffffffffu;
 static_assert(MORE_H_MAX / 8 <= 2 * 512, "two vectors for each of 512 threads");
-constexpr int kMaxParts = 148 * 4;               // CTAs of the backward pass
+constexpr int kStages = 8;                       // tokens on their way to a CTA, at most
+constexpr int kRingBytesPerSm = 200 * 1024;      // bytes of them per SM
+
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar)
+                 : "memory");
+}
 
 __device__ __forceinline__ void widen(const uint4& u, float (&v)[8])
 {
@@ -52,27 +60,84 @@ __device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&v)[8])
     *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// Sums of N values over the threads of a token: a warp (WIDE = false) or the CTA.  buf: N x 32 floats that no other sum uses
-// until another barrier has passed.
+// Eight values as four pairs, for the instructions that work on two at a time.
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b)
+{
+    uint64_t d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ float both(uint64_t a)
+{
+    float x, y;
+    unpack2(a, x, y);
+    return x + y;
+}
+template <class T>
+__device__ __forceinline__ void load8(const T* p, uint64_t (&v)[4])
+{
+    float f[8];
+    load8(p, f);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = pack2(f[2 * i], f[2 * i + 1]);
+}
+template <class T>
+__device__ __forceinline__ void store8(T* p, const uint64_t (&v)[4])
+{
+    float f[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) unpack2(v[i], f[2 * i], f[2 * i + 1]);
+    store8(p, f);
+}
+
+// Sums of three values over a CTA of up to 16 warps, as token_sum<true>: lanes trade values, so that six exchanges do instead of 15.
+__device__ __forceinline__ void token_sum3(float (&v)[3], float (*buf)[16], int warps);
+
+// Sums of N values over the threads of a token: a warp (WIDE = false) or the CTA of up to 16 warps.  buf: N x 16 floats that no other
+// sum uses until another barrier has passed; places of warps that there are not hold zeros.
 template <bool WIDE, int N>
-__device__ __forceinline__ void token_sum(float (&v)[N], float* buf)
+__device__ __forceinline__ void token_sum(float (&v)[N], float (*buf)[16])
 {
 #pragma unroll
     for (int n = 0; n < N; ++n)
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) v[n] += __shfl_xor_sync(kAll, v[n], o);
     if constexpr (WIDE) {
-        const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+        const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
         if (lane == 0)
 #pragma unroll
-            for (int n = 0; n < N; ++n) buf[n * 32 + warp] = v[n];
+            for (int n = 0; n < N; ++n) buf[n][warp] = v[n];
         __syncthreads();
 #pragma unroll
-        for (int n = 0; n < N; ++n) {
-            v[n] = lane < warps ? buf[n * 32 + lane] : 0.f;
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) v[n] += __shfl_xor_sync(kAll, v[n], o);
+        for (int n = 0; n < N; ++n) {                        // (all threads read all parts: shorter than another five shuffles)
+            const float4* q = reinterpret_cast<const float4*>(buf[n]);
+            const float4 a = q[0], b = q[1], c = q[2], d = q[3];
+            v[n] = (((a.x + a.y) + (a.z + a.w)) + ((b.x + b.y) + (b.z + b.w))) + (((c.x + c.y) + (c.z + c.w)) + ((d.x + d.y) + (d.z + d.w)));
         }
+    }
+}
+
+__device__ __forceinline__ void token_sum3(float (&v)[3], float (*buf)[16], int warps)
+{
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const bool up = lane & 16, up8 = lane & 8;
+    float x = (up ? v[1] : v[0]) + __shfl_xor_sync(kAll, up ? v[0] : v[1], 16);
+    const float y = v[2] + __shfl_xor_sync(kAll, v[2], 16);
+    x = (up8 ? y : x) + __shfl_xor_sync(kAll, up8 ? x : y, 8);
+#pragma unroll
+    for (int o = 4; o > 0; o >>= 1) x += __shfl_xor_sync(kAll, x, o);
+    if ((lane & 7) == 0 && lane != 24) buf[up8 ? 2 : up ? 1 : 0][warp] = x;
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < 3; ++n) {
+        const ulonglong2* q = reinterpret_cast<const ulonglong2*>(buf[n]);
+        const ulonglong2 a = q[0], b = q[1];
+        uint64_t s = add2(add2(a.x, a.y), add2(b.x, b.y));
+        if (warps > 8) {
+            const ulonglong2 c = q[2], d = q[3];
+            s = add2(s, add2(add2(c.x, c.y), add2(d.x, d.y)));
+        }
+        v[n] = both(s);
     }
 }
 
@@ -91,7 +156,11 @@ struct CombineParams {
 template <int NV, bool WIDE, class R>
 __global__ void __launch_bounds__(WIDE ? 512 : 256) combine_kernel(const __grid_constant__ CombineParams p)
 {
-    __shared__ float sums[2][32];
+    __shared__ __align__(16) float sums[2][1][16];
+    if (WIDE) {
+        if (threadIdx.x < 32) sums[threadIdx.x >> 4][0][threadIdx.x & 15] = 0.f;
+        __syncthreads();
+    }
     const int lane = WIDE ? threadIdx.x : threadIdx.x & 31, width = WIDE ? blockDim.x : 32;
     const int t = WIDE ? blockIdx.x : blockIdx.x * 8 + (threadIdx.x >> 5);
     if (!WIDE && t >= p.T) return;
@@ -108,7 +177,8 @@ __global__ void __launch_bounds__(WIDE ? 512 : 256) combine_kernel(const __grid_
         if (live[n] && p.residual) load8(static_cast<const R*>(p.residual) + at[n], r[n]);
     }
     if (p.Y) {
-        constexpr int J = NV > 2 ? 2 : 4;                   // slots whose rows are requested at once
+        // slots whose rows are requested at once: for few tokens all 16 of a call are one wait
+        constexpr int J = WIDE && NV == 1 ? 16 : NV > 2 ? 2 : 4;
         for (int j0 = 0; j0 < p.k; j0 += J) {
             uint4 u[J][NV];
             float g[J];
@@ -182,6 +252,125 @@ __global__ void __launch_bounds__(WIDE ? 512 : 256) combine_kernel(const __grid_
     }
 }
 
+// The same for many tokens of long rows: a CTA goes through every gridDim.x-th token, whose rows (the k of them are one piece of memory)
+// come into a ring in shared memory while others are worked on.
+template <int NV, class R>
+__global__ void __launch_bounds__(512) combine_ring_kernel(const __grid_constant__ CombineParams p, int stages, int* status)
+{
+    extern __shared__ __align__(128) uint8_t ring[];
+    __shared__ __align__(16) float sums[2][1][16];
+    __shared__ uint64_t full[kStages];
+    __shared__ int abort_word;
+    volatile int* abort_flag = &abort_word;
+    const int tid = threadIdx.x, width = blockDim.x;
+    const uint32_t rows = p.Y ? (uint32_t)p.k * p.h * 2 : 0u, bytes = rows + (p.residual ? p.h * (uint32_t)sizeof(R) : 0u);
+    auto request = [&](int t, int stage) {
+        const uint32_t bar = smem_u32(&full[stage]), to = smem_u32(ring) + stage * bytes;
+        mbar_expect_tx(bar, bytes);
+        if (p.Y) bulk_load(to, p.Y + (size_t)t * p.k * p.h, rows, bar);
+        if (p.residual) bulk_load(to + rows, static_cast<const R*>(p.residual) + (size_t)t * p.h, bytes - rows, bar);
+    };
+    if (tid < 32) sums[tid >> 4][0][tid & 15] = 0.f;
+    if (tid == 0) {
+        for (int i = 0; i < stages; ++i) mbar_init(smem_u32(&full[i]), 1);
+        abort_word = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        for (int i = 0; i < stages; ++i)
+            if ((long long)blockIdx.x + (long long)i * gridDim.x < p.T) request(blockIdx.x + i * gridDim.x, i);
+    }
+    __syncthreads();
+    uint64_t w_out[NV][4], w_in[NV][4];                      // scale times w_post; w_pre
+#pragma unroll
+    for (int n = 0; n < NV; ++n) {
+        const int c = (n * width + tid) * 8;
+        auto in = [&](int i) { return p.out_x && c < p.h ? p.w_pre[c + i] : 0.f; };
+        auto out = [&](int i) { return c < p.h ? (p.scale ? p.scale[c + i] : 1.f) * (p.w_post ? p.w_post[c + i] : 1.f) : 0.f; };
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            w_out[n][i] = pack2(out(2 * i), out(2 * i + 1));
+            w_in[n][i] = pack2(in(2 * i), in(2 * i + 1));
+        }
+    }
+    // gates of the next token: lane j of every warp has slot j's
+    const int lane = tid & 31;
+    auto gate_of = [&](long long t) { return lane < p.k && t < p.T ? (p.gate ? p.gate[t * p.k + lane] : 1.f) : 0.f; };
+    float next_gate = gate_of(blockIdx.x);
+    int stage = 0;
+    uint32_t phase = 0;
+    for (long long t = blockIdx.x; t < p.T; t += gridDim.x) {
+        const float gates = next_gate;
+        next_gate = gate_of(t + gridDim.x);
+        const bool ok = mbar_wait(smem_u32(&full[stage]), phase, abort_flag, status);    // (given up: goes on, the outputs are undefined)
+        const uint8_t* from = ring + stage * bytes;
+        uint64_t y[NV][4], r[NV][4];
+#pragma unroll
+        for (int n = 0; n < NV; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[n][i] = r[n][i] = pack2(0.f, 0.f);
+        if (p.Y && ok)
+            for (int j = 0; j < p.k; ++j) {
+                const float g = __shfl_sync(kAll, gates, j);
+                if (g == 0.f) continue;                      // (whatever the row holds)
+                const uint64_t g2 = pack2(g, g);
+#pragma unroll
+                for (int n = 0; n < NV; ++n) {
+                    const int c = (n * width + tid) * 8;
+                    if (c >= p.h) continue;
+                    uint64_t v[4];
+                    load8(reinterpret_cast<const __nv_bfloat16*>(from) + (size_t)j * p.h + c, v);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) y[n][i] = fma2(g2, v[i], y[n][i]);
+                }
+            }
+        uint64_t a = pack2(0.f, 0.f);
+#pragma unroll
+        for (int n = 0; n < NV; ++n) {
+            const int c = (n * width + tid) * 8;
+            if (p.residual && ok && c < p.h) load8(reinterpret_cast<const R*>(from + rows) + c, r[n]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) a = fma2(y[n][i], y[n][i], a);
+        }
+        float inv = 1.f;
+        if (p.w_post) {
+            float q[1] = {both(a)};
+            token_sum<true>(q, sums[0]);
+            inv = rsqrtf(fmaf(q[0], p.inv_h, p.eps));
+        } else {
+            __syncthreads();
+        }
+        // (every thread has its part of the stage in registers)
+        if (tid == 0 && ok && t + (long long)stages * gridDim.x < p.T) request((int)(t + (long long)stages * gridDim.x), stage);
+        if (++stage == stages) { stage = 0; phase ^= 1u; }
+        const uint64_t inv2 = pack2(inv, inv);
+        a = pack2(0.f, 0.f);
+#pragma unroll
+        for (int n = 0; n < NV; ++n) {
+            const int c = (n * width + tid) * 8;
+            const bool live = ok && c < p.h;
+            if (p.out_sum && live) store8(p.out_sum + (size_t)t * p.h + c, y[n]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                r[n][i] = fma2(mul2(y[n][i], inv2), w_out[n][i], r[n][i]);
+                a = fma2(r[n][i], r[n][i], a);
+            }
+            if (p.out_residual && live) store8(static_cast<R*>(p.out_residual) + (size_t)t * p.h + c, r[n]);
+        }
+        if (!p.out_x) continue;
+        float q[1] = {both(a)};
+        token_sum<true>(q, sums[1]);
+        inv = rsqrtf(fmaf(q[0], p.inv_h, p.eps));
+        const uint64_t inv_r = pack2(inv, inv);
+#pragma unroll
+        for (int n = 0; n < NV; ++n) {
+            const int c = (n * width + tid) * 8;
+            if (!ok || c >= p.h) continue;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) r[n][i] = mul2(mul2(r[n][i], inv_r), w_in[n][i]);
+            store8(p.out_x + (size_t)t * p.h + c, r[n]);
+        }
+    }
+}
+
 struct CombineBackParams {
     const void* dres;             // [T][h], nullable: zeros
     const __nv_bfloat16* dx;      // [T][h], nullable: zeros
@@ -189,148 +378,148 @@ struct CombineBackParams {
     const void* res;              // [T][h]; read where dx is given
     const float *w_post, *scale, *w_pre;
     float eps, inv_h;
-    int T, h;
+    int T, h, stages;
     void* out_dres;               // nullable
     __nv_bfloat16* out_dsum;      // nullable
     float* parts;                 // [parts][2][h]: S, dw_pre
     int want_parts;
+    int* status;
 };
 
-template <int NV, bool WIDE, class R>
-__global__ void __launch_bounds__(WIDE ? 512 : 256) combine_back_kernel(const __grid_constant__ CombineBackParams p)
+// A CTA goes through every gridDim.x-th token.  The rows of the next tokens are on their way into a ring in shared memory (bulk copies,
+// a row each) while one is worked on: the two sums over a row that have to be known before anything can be written are chains of
+// latency, which left the memory idle half of the time when rows came by loads into registers (519 us at 65536 x 2048, now 284).
+template <int NV, class R, int THREADS>
+__global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) combine_back_kernel(const __grid_constant__ CombineBackParams p)
 {
-    __shared__ float sums[2][4][32];
-    extern __shared__ float columns[];                       // !WIDE: [2][h]
-    const int lane = WIDE ? threadIdx.x : threadIdx.x & 31, width = WIDE ? blockDim.x : 32;
-    const int first = WIDE ? blockIdx.x : blockIdx.x * 8 + (threadIdx.x >> 5), stride = WIDE ? gridDim.x : gridDim.x * 8;
-    float S[NV][8], P[NV][8];
+    extern __shared__ __align__(128) uint8_t ring[];
+    __shared__ __align__(16) float sums[2][3][16];
+    __shared__ uint64_t full[kStages];
+    __shared__ int abort_word;
+    volatile int* abort_flag = &abort_word;
+    const int tid = threadIdx.x, width = blockDim.x;
+    const uint32_t wide = p.h * sizeof(R), narrow = p.h * 2;
+    const uint32_t at_res = p.dres ? wide : 0, at_dx = at_res + (p.dx ? wide : 0), at_sum = at_dx + (p.dx ? narrow : 0), bytes = at_sum + (p.sum ? narrow : 0);
+    auto request = [&](int t, int stage) {
+        const uint32_t bar = smem_u32(&full[stage]), to = smem_u32(ring) + stage * bytes;
+        const size_t row = (size_t)t * p.h;
+        mbar_expect_tx(bar, bytes);
+        if (p.dres) bulk_load(to, static_cast<const R*>(p.dres) + row, wide, bar);
+        if (p.dx) {
+            bulk_load(to + at_res, static_cast<const R*>(p.res) + row, wide, bar);
+            bulk_load(to + at_dx, p.dx + row, narrow, bar);
+        }
+        if (p.sum) bulk_load(to + at_sum, p.sum + row, narrow, bar);
+    };
+    for (int i = tid; i < 2 * 3 * 16; i += width) (&sums[0][0][0])[i] = 0.f;
+    if (tid == 0) {
+        for (int i = 0; i < p.stages; ++i) mbar_init(smem_u32(&full[i]), 1);
+        abort_word = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        for (int i = 0; i < p.stages; ++i)
+            if ((long long)blockIdx.x + (long long)i * gridDim.x < p.T) request(blockIdx.x + i * gridDim.x, i);
+    }
+    __syncthreads();
+    uint64_t S[NV][4], P[NV][4], w_in[NV][4], w_out[NV][4];  // column sums; w_pre, and scale times w_post
 #pragma unroll
-    for (int n = 0; n < NV; ++n)
+    for (int n = 0; n < NV; ++n) {
+        const int c = (n * width + tid) * 8;
+        auto in = [&](int i) { return p.dx && c < p.h ? p.w_pre[c + i] : 0.f; };
+        auto out = [&](int i) { return c < p.h ? (p.scale ? p.scale[c + i] : 1.f) * (p.w_post ? p.w_post[c + i] : 1.f) : 0.f; };
 #pragma unroll
-        for (int i = 0; i < 8; ++i) S[n][i] = P[n][i] = 0.f;
-    for (int t = first; t < p.T; t += stride) {
-        float g[NV][8], r[NV][8], d[NV][8], y[NV][8];
-        bool live[NV];
+        for (int i = 0; i < 4; ++i) {
+            S[n][i] = P[n][i] = pack2(0.f, 0.f);
+            w_in[n][i] = pack2(in(2 * i), in(2 * i + 1));
+            w_out[n][i] = pack2(out(2 * i), out(2 * i + 1));
+        }
+    }
+    const int warps = width >> 5;
+    int stage = 0;
+    uint32_t phase = 0;
+    for (long long t = blockIdx.x; t < p.T; t += gridDim.x) {
+        const bool ok = mbar_wait(smem_u32(&full[stage]), phase, abort_flag, p.status);   // (given up: goes on, the outputs are undefined)
+        const uint8_t* from = ring + stage * bytes;
+        uint64_t g[NV][4], r[NV][4], v[NV][4], d[NV][4], y[NV][4];
         float q[3] = {0.f, 0.f, 0.f};                        // sums of r^2, r v, y^2
 #pragma unroll
         for (int n = 0; n < NV; ++n) {
-            const int c = (n * width + lane) * 8;
-            const size_t at = (size_t)t * p.h + c;
-            live[n] = c < p.h;
+            const int c = (n * width + tid) * 8;
+            const bool live = ok && c < p.h;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) g[n][i] = r[n][i] = d[n][i] = y[n][i] = 0.f;
-            if (!live[n]) continue;
-            if (p.dres) load8(static_cast<const R*>(p.dres) + at, g[n]);
-            if (p.dx) {
-                load8(static_cast<const R*>(p.res) + at, r[n]);
-                load8(p.dx + at, d[n]);
-            }
-            if (p.sum) load8(p.sum + at, y[n]);
-        }
-#pragma unroll
-        for (int n = 0; n < NV; ++n) {
-            if (!live[n]) continue;
-            float w[8];
-            if (p.dx) {
-                load8(p.w_pre + (n * width + lane) * 8, w);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    q[0] = fmaf(r[n][i], r[n][i], q[0]);
-                    q[1] = fmaf(r[n][i], d[n][i] * w[i], q[1]);
+            for (int i = 0; i < 4; ++i) g[n][i] = r[n][i] = d[n][i] = y[n][i] = pack2(0.f, 0.f);
+            if (live) {
+                if (p.dres) load8(reinterpret_cast<const R*>(from) + c, g[n]);
+                if (p.dx) {
+                    load8(reinterpret_cast<const R*>(from + at_res) + c, r[n]);
+                    load8(reinterpret_cast<const __nv_bfloat16*>(from + at_dx) + c, d[n]);
                 }
+                if (p.sum) load8(reinterpret_cast<const __nv_bfloat16*>(from + at_sum) + c, y[n]);
+            }
+            uint64_t a[3] = {pack2(0.f, 0.f), pack2(0.f, 0.f), pack2(0.f, 0.f)};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                v[n][i] = mul2(d[n][i], w_in[n][i]);
+                a[0] = fma2(r[n][i], r[n][i], a[0]);
+                a[1] = fma2(r[n][i], v[n][i], a[1]);
+                a[2] = fma2(y[n][i], y[n][i], a[2]);
             }
 #pragma unroll
-            for (int i = 0; i < 8; ++i) q[2] = fmaf(y[n][i], y[n][i], q[2]);
+            for (int i = 0; i < 3; ++i) q[i] += both(a[i]);
         }
-        token_sum<WIDE>(q, sums[0][0]);
+        token_sum3(q, sums[0], warps);
+        // (every thread has its part of the stage in registers)
+        if (tid == 0 && ok && t + (long long)p.stages * gridDim.x < p.T) request((int)(t + (long long)p.stages * gridDim.x), stage);
+        if (++stage == p.stages) { stage = 0; phase ^= 1u; }
         const float inv = rsqrtf(fmaf(q[0], p.inv_h, p.eps)), mean = q[1] * inv * p.inv_h;       // mean of rh v
         const float inv_y = p.w_post ? rsqrtf(fmaf(q[2], p.inv_h, p.eps)) : 1.f;
+        const uint64_t inv2 = pack2(inv, inv), less = pack2(-mean, -mean), inv_y2 = pack2(inv_y, inv_y);
         float m[1] = {0.f};                                  // sum of yh u
 #pragma unroll
         for (int n = 0; n < NV; ++n) {
-            const int c = (n * width + lane) * 8;
-            if (!live[n]) continue;
-            float w[8];
-            if (p.dx) {
-                load8(p.w_pre + c, w);
+            const int c = (n * width + tid) * 8;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float rh = r[n][i] * inv;
-                    P[n][i] = fmaf(d[n][i], rh, P[n][i]);
-                    g[n][i] = fmaf(inv, fmaf(d[n][i], w[i], -rh * mean), g[n][i]);
-                }
+            for (int i = 0; i < 4; ++i) {                    // (without dx: zeros)
+                const uint64_t rh = mul2(r[n][i], inv2);
+                P[n][i] = fma2(d[n][i], rh, P[n][i]);
+                g[n][i] = fma2(inv2, fma2(rh, less, v[n][i]), g[n][i]);
             }
-            if (p.out_dres) store8(static_cast<R*>(p.out_dres) + (size_t)t * p.h + c, g[n]);
+            if (p.out_dres && ok && c < p.h) store8(static_cast<R*>(p.out_dres) + (size_t)t * p.h + c, g[n]);
+            uint64_t a = pack2(0.f, 0.f);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                y[n][i] *= inv_y;
-                S[n][i] = fmaf(g[n][i], y[n][i], S[n][i]);
+            for (int i = 0; i < 4; ++i) {
+                y[n][i] = mul2(y[n][i], inv_y2);
+                S[n][i] = fma2(g[n][i], y[n][i], S[n][i]);
+                g[n][i] = mul2(g[n][i], w_out[n][i]);
+                a = fma2(g[n][i], y[n][i], a);
             }
-            if (p.scale) {
-                load8(p.scale + c, w);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) g[n][i] *= w[i];
-            }
-            if (p.w_post) {
-                load8(p.w_post + c, w);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    g[n][i] *= w[i];
-                    m[0] = fmaf(g[n][i], y[n][i], m[0]);
-                }
-            }
+            m[0] += both(a);
         }
         if (p.out_dsum) {
             float mean_y = 0.f;
             if (p.w_post) {
-                token_sum<WIDE>(m, sums[1][0]);
+                token_sum<true>(m, sums[1]);
                 mean_y = m[0] * p.inv_h;
             }
+            const uint64_t less_y = pack2(-mean_y, -mean_y);
 #pragma unroll
             for (int n = 0; n < NV; ++n) {
-                if (!live[n]) continue;
+                const int c = (n * width + tid) * 8;
+                if (!ok || c >= p.h) continue;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) g[n][i] = inv_y * fmaf(-y[n][i], mean_y, g[n][i]);
-                store8(p.out_dsum + (size_t)t * p.h + (n * width + lane) * 8, g[n]);
+                for (int i = 0; i < 4; ++i) g[n][i] = mul2(inv_y2, fma2(y[n][i], less_y, g[n][i]));
+                store8(p.out_dsum + (size_t)t * p.h + c, g[n]);
             }
         }
-        if constexpr (WIDE)
-            if (!(p.out_dsum && p.w_post)) __syncthreads();  // the next token's first sum may overwrite this one's
+        if (!(p.out_dsum && p.w_post)) __syncthreads();      // the next token's first sum may overwrite this one's
     }
     if (!p.want_parts) return;
     float* out = p.parts + (size_t)blockIdx.x * 2 * p.h;
-    if constexpr (WIDE) {
 #pragma unroll
-        for (int n = 0; n < NV; ++n) {
-            const int c = (n * width + lane) * 8;
-            if (c < p.h) {
-                store8(out + c, S[n]);
-                store8(out + p.h + c, P[n]);
-            }
-        }
-    } else {
-        for (int w = 0; w < 8; ++w) {                        // the CTA's warps in turn
-            if ((int)(threadIdx.x >> 5) == w)
-#pragma unroll
-                for (int n = 0; n < NV; ++n) {
-                    const int c = (n * width + lane) * 8;
-                    if (c >= p.h) continue;
-                    float a[8], b[8];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) a[i] = b[i] = 0.f;
-                    if (w > 0) {
-                        load8(columns + c, a);
-                        load8(columns + p.h + c, b);
-                    }
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        a[i] += S[n][i];
-                        b[i] += P[n][i];
-                    }
-                    store8(w < 7 ? columns + c : out + c, a);
-                    store8(w < 7 ? columns + p.h + c : out + p.h + c, b);
-                }
-            __syncthreads();
+    for (int n = 0; n < NV; ++n) {
+        const int c = (n * width + tid) * 8;
+        if (c < p.h) {
+            store8(out + c, S[n]);
+            store8(out + p.h + c, P[n]);
         }
     }
 }
@@ -342,8 +531,16 @@ __global__ void __launch_bounds__(1024) combine_columns_kernel(const float* __re
     __shared__ float buf[32][33];
     const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5, c = blockIdx.x * 32 + tx;        // c in [0, 2 h)
     float v = 0.f;
-    if (c < 2 * h)
-        for (int i = ty; i < count; i += 32) v += parts[(size_t)i * 2 * h + c];
+    if (c < 2 * h) {
+        int i = ty;
+        for (; i + 96 < count; i += 128) {                   // (four loads in flight; the order of the sum is fixed all the same)
+            float a[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) a[j] = parts[(size_t)(i + 32 * j) * 2 * h + c];
+            v += (a[0] + a[1]) + (a[2] + a[3]);
+        }
+        for (; i < count; i += 32) v += parts[(size_t)i * 2 * h + c];
+    }
     buf[ty][tx] = v;
     __syncthreads();
     if (ty != 0 || c >= 2 * h) return;
@@ -363,34 +560,72 @@ struct Spread {
     int nv, width;
     bool wide;
 };
-Spread spread(int T, int h, bool backward)
+Spread spread(int T, int h)
 {
     const int vecs = h / 8;
     Spread s;
-    s.wide = vecs > (backward ? 64 : 128) || T <= 148 * 8;       // (few tokens: as many loads at once as there are)
+    s.wide = vecs > 128 || T <= 148 * 8;                         // (few tokens: as many loads at once as there are)
     if (!s.wide) {
         s.width = 32;
         s.nv = vecs <= 32 ? 1 : (vecs <= 64 ? 2 : 4);
         return s;
     }
     s.nv = T <= 148 * 8 && vecs <= 512 ? 1 : 2;                  // (at most 512 threads: MORE_H_MAX / 16)
-
     s.width = ((vecs + s.nv - 1) / s.nv + 31) / 32 * 32;
     return s;
 }
 
-bool misaligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
-
-int backward_parts(int T, int h)
+// The backward pass: threads and vectors per thread, CTAs per SM (about 512 threads of them: with 768 at 85 registers values spill, and
+// what the rings leave of the L1 cache makes that slow, 322 us against 290 at 65536 x 2048), CTAs.
+struct BackPlan {
+    int nv, width, per_sm, ctas;
+};
+BackPlan plan_back(int T, int h)
 {
-    const long long want = spread(T, h, true).wide ? T : (T + 7) / 8;
-    return (int)(want < kMaxParts ? want : kMaxParts);
+    const int vecs = h / 8;
+    BackPlan b;
+    b.nv = vecs <= 512 ? 1 : 2;
+    b.width = ((vecs + b.nv - 1) / b.nv + 31) / 32 * 32;
+    b.per_sm = 512 / b.width;
+    if (b.per_sm > 8) b.per_sm = 8;
+    b.ctas = T < 148 * b.per_sm ? T : 148 * b.per_sm;
+    return b;
 }
 
-template <int NV, bool WIDE, class R>
-void launch_back(const CombineBackParams& p, int blocks, int width, cudaStream_t st)
+bool misaligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
+
+// The ring: stages of `token` bytes for each of per_sm CTAs, which becomes fewer where two do not fit.  0: not even for one.
+int ring_stages(size_t token, int* per_sm)
 {
-    combine_back_kernel<NV, WIDE, R><<<blocks, WIDE ? width : 256, WIDE ? 0 : 2 * p.h * sizeof(float), st>>>(p);
+    while (*per_sm > 1 && kRingBytesPerSm / *per_sm < 2 * token) --*per_sm;
+    const size_t n = kRingBytesPerSm / *per_sm / token;
+    return n < 2 ? 0 : n > kStages ? kStages : (int)n;
+}
+template <int NV, class R, int THREADS>
+int launch_back(CombineBackParams p, const BackPlan& b, cudaStream_t st)
+{
+    const size_t token = (size_t)p.h * ((p.dres ? sizeof(R) : 0) + (p.dx ? sizeof(R) + 2 : 0) + (p.sum ? 2 : 0));
+    int per_sm = b.per_sm;
+    p.stages = ring_stages(token, &per_sm);                          // (two of the longest rows, 96 KB each, fit)
+    const size_t smem = p.stages * token;
+    if (cudaFuncSetAttribute(combine_back_kernel<NV, R, THREADS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return MORE_ERR_CUDA;
+    combine_back_kernel<NV, R, THREADS><<<b.ctas, b.width, smem, st>>>(p);
+    return MORE_OK;
+}
+template <int NV, class R>
+int launch_ring(const CombineParams& p, int* status, cudaStream_t st, bool* done)
+{
+    const size_t token = (size_t)p.h * ((p.Y ? 2 * (size_t)p.k : 0) + (p.residual ? sizeof(R) : 0));
+    const int width = ((p.h / 8 + NV - 1) / NV + 31) / 32 * 32;
+    int per_sm = 512 / width > 8 ? 8 : 512 / width;
+    const int stages = ring_stages(token, &per_sm);
+    *done = stages > 0;
+    if (!*done) return MORE_OK;
+    const int ctas = p.T < 148 * per_sm ? p.T : 148 * per_sm;
+    const size_t smem = stages * token;
+    if (cudaFuncSetAttribute(combine_ring_kernel<NV, R>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return MORE_ERR_CUDA;
+    combine_ring_kernel<NV, R><<<ctas, width, smem, st>>>(p, stages, status);
+    return MORE_OK;
 }
 template <int NV, bool WIDE, class R>
 void launch_forward(const CombineParams& p, int width, cudaStream_t st)
@@ -417,18 +652,25 @@ int more_combine(const void* Y, const float* gate, const void* residual, int res
         misaligned(w_pre, 16) || misaligned(out_residual, 16) || misaligned(out_x, 16) || misaligned(out_sum, 16))
         return MORE_ERR_ALIGN;
     DeviceCtx* ctx = nullptr;
-    const int rc = device_ctx(&ctx);
-    if (rc != MORE_OK) return rc;
+    const int found = device_ctx(&ctx);
+    if (found != MORE_OK) return found;
     CombineParams p;
     p.Y = static_cast<const __nv_bfloat16*>(Y); p.gate = gate; p.residual = residual;
     p.w_post = Y ? w_post : nullptr; p.scale = Y ? scale : nullptr; p.w_pre = w_pre;      // (nothing to join: the next block's norm alone)
     p.eps = eps; p.inv_h = 1.f / (float)h; p.T = T; p.h = h; p.k = k;
     p.out_residual = out_residual; p.out_x = static_cast<__nv_bfloat16*>(out_x); p.out_sum = static_cast<__nv_bfloat16*>(out_sum);
-    const Spread sp = spread(T, h, false);
+    const Spread sp = spread(T, h);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const bool f32 = residual_type == MORE_RESIDUAL_FP32;
 #define MORE_FORWARD(NV, WIDE) (f32 ? launch_forward<NV, WIDE, float>(p, sp.width, st) : launch_forward<NV, WIDE, __nv_bfloat16>(p, sp.width, st))
-    if (sp.wide) sp.nv == 1 ? MORE_FORWARD(1, true) : MORE_FORWARD(2, true);
+    bool done = false;
+    if (T > 148 * 8 && h >= 1024) {                                  // (two stages of the rows of 24 slots or more may not fit)
+        const int rc = h <= 4096 ? (f32 ? launch_ring<1, float>(p, ctx->status, st, &done) : launch_ring<1, __nv_bfloat16>(p, ctx->status, st, &done))
+                                 : (f32 ? launch_ring<2, float>(p, ctx->status, st, &done) : launch_ring<2, __nv_bfloat16>(p, ctx->status, st, &done));
+        if (rc != MORE_OK) return rc;
+    }
+    if (done) {
+    } else if (sp.wide) sp.nv == 1 ? MORE_FORWARD(1, true) : MORE_FORWARD(2, true);
     else sp.nv == 1 ? MORE_FORWARD(1, false) : (sp.nv == 2 ? MORE_FORWARD(2, false) : MORE_FORWARD(4, false));
 #undef MORE_FORWARD
     count_launch(1);
@@ -438,7 +680,7 @@ int more_combine(const void* Y, const float* gate, const void* residual, int res
 long long more_combine_workspace(int T, int h)
 {
     if (T < 0 || h < 8 || h % 8 != 0 || h > MORE_H_MAX) return MORE_ERR_SHAPE;
-    return T == 0 ? 0 : (long long)backward_parts(T, h) * 2 * h * (long long)sizeof(float);
+    return T == 0 ? 0 : (long long)plan_back(T, h).ctas * 2 * h * (long long)sizeof(float);
 }
 
 int more_combine_backward(const void* dresidual, const void* dx, const void* sum, const void* residual_out, int residual_type,
@@ -464,7 +706,8 @@ int more_combine_backward(const void* dresidual, const void* dx, const void* sum
     const int rc = device_ctx(&ctx);
     if (rc != MORE_OK) return rc;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const int parts = T > 0 ? backward_parts(T, h) : 0;
+    const BackPlan plan = plan_back(T, h);
+    const int parts = plan.ctas;
     if (T > 0) {
         CombineBackParams p;
         p.dres = dresidual; p.dx = static_cast<const __nv_bfloat16*>(dx); p.sum = static_cast<const __nv_bfloat16*>(sum); p.res = residual_out;
@@ -472,12 +715,12 @@ int more_combine_backward(const void* dresidual, const void* dx, const void* sum
         p.eps = eps; p.inv_h = 1.f / (float)h; p.T = T; p.h = h;
         p.out_dres = out_dresidual; p.out_dsum = static_cast<__nv_bfloat16*>(out_dsum);
         p.parts = static_cast<float*>(workspace); p.want_parts = columns;
-        const Spread sp = spread(T, h, true);
+        p.status = ctx->status;
         const bool f32 = residual_type == MORE_RESIDUAL_FP32;
-#define MORE_BACK(NV, WIDE) (f32 ? launch_back<NV, WIDE, float>(p, parts, sp.width, st) : launch_back<NV, WIDE, __nv_bfloat16>(p, parts, sp.width, st))
-        if (sp.wide) sp.nv == 1 ? MORE_BACK(1, true) : MORE_BACK(2, true);
-        else sp.nv == 1 ? MORE_BACK(1, false) : (sp.nv == 2 ? MORE_BACK(2, false) : MORE_BACK(4, false));
-#undef MORE_BACK
+        const int done = plan.nv == 2       ? (f32 ? launch_back<2, float, 512>(p, plan, st) : launch_back<2, __nv_bfloat16, 512>(p, plan, st))
+                         : plan.width > 256 ? (f32 ? launch_back<1, float, 512>(p, plan, st) : launch_back<1, __nv_bfloat16, 512>(p, plan, st))
+                                            : (f32 ? launch_back<1, float, 256>(p, plan, st) : launch_back<1, __nv_bfloat16, 256>(p, plan, st));
+        if (done != MORE_OK) return done;
         count_launch(1);
         if (cudaGetLastError() != cudaSuccess) return MORE_ERR_CUDA;
     }
