@@ -392,6 +392,7 @@ struct CombineBackParams {
 template <int NV, class R, int THREADS>
 __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) combine_back_kernel(const __grid_constant__ CombineBackParams p)
 {
+    let_next_begin();
     extern __shared__ __align__(128) uint8_t ring[];
     __shared__ __align__(16) float sums[2][3][16];
     __shared__ uint64_t full[kStages];
@@ -528,6 +529,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) combine_back_
 __global__ void __launch_bounds__(1024) combine_columns_kernel(const float* __restrict__ parts, int count, int h, const float* __restrict__ w_post,
                                                                 const float* __restrict__ scale, float* out_dw_post, float* out_dscale, float* out_dw_pre)
 {
+    wait_for_previous();
     __shared__ float buf[32][33];
     const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5, c = blockIdx.x * 32 + tx;        // c in [0, 2 h)
     float v = 0.f;
@@ -725,8 +727,9 @@ int more_combine_backward(const void* dresidual, const void* dx, const void* sum
         if (cudaGetLastError() != cudaSuccess) return MORE_ERR_CUDA;
     }
     if (columns) {
-        combine_columns_kernel<<<(2 * h + 31) / 32, 1024, 0, st>>>(static_cast<const float*>(workspace), parts, h, w_post, scale, out_dw_post,
-                                                                  out_dscale, out_dw_pre);
+        if (launch_behind(combine_columns_kernel, (2 * h + 31) / 32, 1024, 0, st, static_cast<const float*>(workspace), parts, h, w_post, scale,
+                          out_dw_post, out_dscale, out_dw_pre) != cudaSuccess)
+            return MORE_ERR_CUDA;
         count_launch(1);
     }
     return cudaGetLastError() == cudaSuccess ? MORE_OK : MORE_ERR_CUDA;

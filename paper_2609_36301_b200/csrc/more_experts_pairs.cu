@@ -12,7 +12,6 @@ namespace more {
 namespace {
 
 constexpr int kPThreads = 256;
-constexpr int kBatch = 8;                         // 16-byte loads in flight per thread
 
 __device__ __forceinline__ float ld_cluster(uint32_t addr, int rank)
 {
@@ -40,6 +39,7 @@ __device__ __forceinline__ uint4 ld_stream(const __nv_bfloat16* p)      // weigh
 }
 
 // Threads as `groups` column groups of 8 times as many row groups as fit: acc = sum over this thread's rows of x[row] W[row][8 columns].
+template <int kBatch>                             // 16-byte loads in flight per thread, twice
 struct Slice {
     const __nv_bfloat16* at;      // of this thread's first row, or nullptr
     size_t step;                  // elements between its rows
@@ -79,7 +79,9 @@ __device__ __forceinline__ float column_sum(const float* red, int cols, int row_
     return v;
 }
 
-__global__ void __launch_bounds__(kPThreads)
+// BATCH, PER_SM: what a CTA has in flight, and how many of them are resident.
+template <int BATCH, int PER_SM>
+__global__ void __launch_bounds__(kPThreads, PER_SM)
 pairs_kernel(const __nv_bfloat16* __restrict__ X, const __nv_bfloat16* __restrict__ W1, const __nv_bfloat16* __restrict__ W2,
              const int32_t* __restrict__ idx, int h, int s, int M, int k, int ranks, __nv_bfloat16* __restrict__ Y)
 {
@@ -97,11 +99,11 @@ pairs_kernel(const __nv_bfloat16* __restrict__ X, const __nv_bfloat16* __restric
     // first product: columns in passes of up to 256 groups of 8
     const __nv_bfloat16* w1 = W1 + ((size_t)e * h + v0 * 8) * 2 * s;
     const int all = s / 4;
-    uint4 w[kBatch];
+    uint4 w[BATCH];
     for (int g0 = 0; g0 < all; g0 += kPThreads) {
         const int groups = min(all - g0, kPThreads), rg = kPThreads / groups;
         const int mine = tid / groups, col = (g0 + tid % groups) * 8;
-        Slice sl{mine < rg ? w1 + (size_t)mine * 2 * s + col : nullptr, (size_t)rg * 2 * s, rows, mine, rg};
+        Slice<BATCH> sl{mine < rg ? w1 + (size_t)mine * 2 * s + col : nullptr, (size_t)rg * 2 * s, rows, mine, rg};
         sl.load(w, 0);
         if (g0 == 0) {
             const __nv_bfloat16* from = X + (size_t)(pair / k) * h + v0 * 8;
@@ -123,7 +125,7 @@ pairs_kernel(const __nv_bfloat16* __restrict__ X, const __nv_bfloat16* __restric
     auto slice2 = [&](int g0) {
         const int groups = min(vn - g0, kPThreads), rg = groups > 0 ? kPThreads / groups : 0;
         const int mine = groups > 0 ? tid / groups : 0;
-        return Slice{mine < rg ? W2 + ((size_t)e * s + mine) * h + (size_t)(v0 + g0 + tid % groups) * 8 : nullptr, (size_t)rg * h, s, mine, rg};
+        return Slice<BATCH>{mine < rg ? W2 + ((size_t)e * s + mine) * h + (size_t)(v0 + g0 + tid % groups) * 8 : nullptr, (size_t)rg * h, s, mine, rg};
     };
     if (passes > 0) slice2(0).load(w, 0);
     cluster_wait();
@@ -140,7 +142,7 @@ pairs_kernel(const __nv_bfloat16* __restrict__ X, const __nv_bfloat16* __restric
     cluster_arrive();                                  // (done with the other CTAs' parts)
     for (int p = 0; p < passes; ++p) {
         const int g0 = p * kPThreads, groups = min(vn - g0, kPThreads), rg = kPThreads / groups;
-        const Slice sl = slice2(g0);
+        const Slice<BATCH> sl = slice2(g0);
         if (p > 0) sl.load(w, 0);
         float acc[8] = {};
         sl.sum(acc, w, act);
@@ -162,11 +164,16 @@ pairs_kernel(const __nv_bfloat16* __restrict__ X, const __nv_bfloat16* __restric
 int launch_experts_pairs(const ExpertsArgs& a, const DeviceCtx& ctx)
 {
     const long long P = (long long)a.T * a.k;
-    // CTAs per pair: as many as fill the SMs, but not less than 8 rows each
+    // CTAs per pair: as many as are resident at once, two per SM, but not fewer than 32 rows each.  (8 pairs of h = 2048, s = 64: 38 us
+    // with one CTA each, 9.2 with eight; 64: 38, 16.7 with four, 21 with eight; 512: 90, 96 with two, 111 with four.)
     int ranks = 1;
-    while (ranks < 8 && P * ranks < 2LL * ctx.sm_count && a.h / (ranks * 2) >= 32) ranks *= 2;
+    while (ranks < 8 && P * ranks * 2 <= 2LL * ctx.sm_count && a.h / (ranks * 2) >= 32) ranks *= 2;
     const size_t smem = sizeof(float) * (kPThreads * 8 + 3 * (size_t)a.s + ((size_t)a.h / 8 + ranks - 1) / ranks * 8);
-    if (cudaFuncSetAttribute(pairs_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return MORE_ERR_CUDA;
+    // More pairs than two CTAs per SM hold at once: four smaller ones (512 pairs of h = 2048, s = 64: 72 us instead of 90; for fewer
+    // pairs they are slower, 8: 11.3 instead of 9.2, 128 of h = 4096, s = 128: 108 instead of 84).
+    const bool many = P > 2LL * ctx.sm_count;
+    auto kern = many ? pairs_kernel<4, 4> : pairs_kernel<8, 2>;
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return MORE_ERR_CUDA;
     if (P * ranks > 0x7fffffffLL) return MORE_ERR_TOO_LARGE;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(P * ranks));
@@ -179,7 +186,7 @@ int launch_experts_pairs(const ExpertsArgs& a, const DeviceCtx& ctx)
     at.val.clusterDim.y = at.val.clusterDim.z = 1;
     cfg.attrs = &at;
     cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, pairs_kernel, a.X, a.W1, a.W2, a.idx, a.h, a.s, a.M, a.k, ranks, a.out_y) != cudaSuccess) return MORE_ERR_CUDA;
+    if (cudaLaunchKernelEx(&cfg, kern, a.X, a.W1, a.W2, a.idx, a.h, a.s, a.M, a.k, ranks, a.out_y) != cudaSuccess) return MORE_ERR_CUDA;
     count_launch(1);
     return cudaGetLastError() == cudaSuccess ? MORE_OK : MORE_ERR_CUDA;
 }

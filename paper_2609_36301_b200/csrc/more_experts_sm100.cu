@@ -25,6 +25,8 @@
 // to the second product as bf16 rows in expert order (s of them against h of an output row).
 #include "more_experts.cuh"
 
+#include <math.h>
+
 namespace more {
 
 namespace {
@@ -166,6 +168,7 @@ struct Ring {
 // tiles[0].x is how many there are.  Every CTA takes 1024 experts and counts the tiles of all experts before them itself.
 __global__ void __launch_bounds__(1024) tiles_kernel(const int32_t* __restrict__ offsets, int M, int P, int capacity, int4* __restrict__ tiles)
 {
+    let_next_begin();
     __shared__ int warp_sum[32];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     auto run = [&](int e, int& lo) {                        // (whatever the offsets hold, a run stays within the places)
@@ -410,7 +413,9 @@ rows_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUte
     uint8_t* const staging_at = smem_raw + (ring - smem_u32(smem_raw)) + kXRing;
     Control* ctl = reinterpret_cast<Control*>(staging_at + kXStaging);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    let_next_begin();
     const uint32_t tmem = open_cta(ctl, kCompute ? 8 : 4, warp);
+    wait_for_previous();
     volatile int* abort_flag = &ctl->abort;
     const int units = p.tiles[0].x * p.chunks;
 
@@ -750,7 +755,9 @@ weights_kernel(const __grid_constant__ CUtensorMap mtoken, const __grid_constant
     uint8_t* const staging_at = smem_raw + (ring - smem_u32(smem_raw)) + kXRing;
     Control* ctl = reinterpret_cast<Control*>(staging_at + kXStaging);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    let_next_begin();
     const uint32_t tmem = open_cta(ctl, 8, warp);
+    wait_for_previous();
     volatile int* abort_flag = &ctl->abort;
 
     if (warp == 0 || warp >= 10) {
@@ -891,6 +898,8 @@ struct JoinParams {
 };
 __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ JoinParams p)
 {
+    let_next_begin();
+    wait_for_previous();
     const int vecs = p.h / 8;
     const long long all = p.out_dx ? (long long)p.T * vecs : 0;
     const long long first = (long long)blockIdx.x * 256 + threadIdx.x, stride = (long long)gridDim.x * 256;
@@ -988,9 +997,10 @@ int launch_rows(const CUtensorMap& ma, const CUtensorMap& mw, RowsParams p, long
     const long long units = tiles * p.chunks;
     if (units > 0x7fff0000LL) return MORE_ERR_TOO_LARGE;
     const int grid = units < ctx.sm_count ? (int)units : ctx.sm_count;
-    rows_kernel<MODE><<<grid, threads_of(MODE == kUp || MODE == kBackAct ? kLoaders : kFewLoaders), kXSmem, st>>>(ma, mw, p);
+    const int threads = threads_of(MODE == kUp || MODE == kBackAct ? kLoaders : kFewLoaders);
+    if (launch_behind(rows_kernel<MODE>, grid, threads, kXSmem, st, ma, mw, p) != cudaSuccess) return MORE_ERR_CUDA;
     count_launch(1);
-    return cudaGetLastError() == cudaSuccess ? MORE_OK : MORE_ERR_CUDA;
+    return MORE_OK;
 }
 
 int launch_tiles(const ExpertsArgs& a, cudaStream_t st)
@@ -1014,9 +1024,10 @@ int launch_weights(const CUtensorMap& mtoken, const CUtensorMap (&mplace)[2], We
     const long long units = (long long)p.M * p.mtiles * p.chunks;
     if (units > 0x7fff0000LL) return MORE_ERR_TOO_LARGE;
     const int grid = units < ctx.sm_count ? (int)units : ctx.sm_count;
-    weights_kernel<<<grid, threads_of(kLoaders), kXSmem, st>>>(mtoken, mplace[0], mplace[1], mout, p);
+    if (launch_behind(weights_kernel, grid, threads_of(kLoaders), kXSmem, st, mtoken, mplace[0], mplace[1], mout, p) != cudaSuccess)
+        return MORE_ERR_CUDA;
     count_launch(1);
-    return cudaGetLastError() == cudaSuccess ? MORE_OK : MORE_ERR_CUDA;
+    return MORE_OK;
 }
 
 int launch_experts(const ExpertsArgs& a, const DeviceCtx& ctx)
@@ -1102,9 +1113,8 @@ int launch_experts_backward(const ExpertsArgs& a, const DeviceCtx& ctx)
         j.out_dx = a.out_dx; j.out_dgate = a.out_dgate;
         const long long items = a.out_dx ? (long long)a.T * (a.h / 8) : P;
         const long long blocks = (items + 255) / 256;
-        join_kernel<<<(int)(blocks < 148 * 16 ? blocks : 148 * 16), 256, 0, a.stream>>>(j);
+        if (launch_behind(join_kernel, (int)(blocks < 148 * 16 ? blocks : 148 * 16), 256, 0, a.stream, j) != cudaSuccess) return MORE_ERR_CUDA;
         count_launch(1);
-        if (cudaGetLastError() != cudaSuccess) return MORE_ERR_CUDA;
     }
     WeightsParams q{};
     q.offsets = a.offsets; q.pairs = a.pairs; q.P = (int)P; q.T = a.T; q.by_k.by(a.k); q.M = a.M;
@@ -1128,6 +1138,26 @@ int check_sizes(int T, int h, int s, int M, int k)
     if (M < 1 || M > MORE_M_MAX || k < 1 || k > MORE_K_MAX || k > M) return MORE_ERR_SHAPE;
     if ((long long)T * k > 0x7fffffffLL) return MORE_ERR_TOO_LARGE;            // pairs are named by int32 positions
     return MORE_OK;
+}
+
+// Which forward path.  Pairs read their expert's weights each, 8 us behind a start (20 GB/s per CTA, 6.2 TB/s in all).  Tiles read those
+// of the experts that are hit, of evenly spread ids M (1 - exp(-P / M)), 24 us behind for three kernels; a kernel takes the bytes'
+// time (100 GB/s per unit, 6.2 TB/s in all) or that of its stages, 0.35 us each of the first, 0.8 of the second, over the SMs.
+// Measured on eight combinations of h, s and M from 8 to 8192 pairs (us, pairs / tiles): h = 2048, s = 64, M = 8192: 12 / 31 at 8
+// pairs, 76 / 84 at 512, 141 / 135 at 1024, 266 / 231 at 2048; h = 512, s = 64, M = 64: 14 / 25 at 128, 25 / 25 at 512, 41 / 25
+// at 1024; h = 4096, s = 512, M = 16: 72 / 51 at 8.  The choice cost 4 % at worst there.
+int cheaper_path(int T, int h, int s, int M, int k)
+{
+    const double P = (double)T * k, weights = 6.0 * h * s, sms = 148, most = 6.2e6;     // bytes; bytes per us
+    const double hit = M * -expm1(-P / M);
+    double ctas = P;                                                 // as launch_experts_pairs has them
+    for (int ranks = 1; ranks < 8 && ctas * 2 <= 2 * sms && h / (ranks * 2) >= 32; ranks *= 2) ctas *= 2;
+    const double pairs = 8 + P * (0.009 + weights / fmin(most, fmin(ctas, 2 * sms) * 20e3));
+    const double wide = (s + 127) / 128, rate = fmin(most, hit * wide * 100e3);
+    const double up = hit * fmax(weights * 2 / 3 / rate, wide * ((h + 63) / 64) * 0.35 / sms);
+    const double down = hit * fmax(weights / 3 / rate, ((h + 255) / 256) * ((s + 63) / 64) * 0.8 / sms);
+    const double tiles = 24 + up + down;
+    return pairs <= tiles ? MORE_EXPERTS_PAIRS : MORE_EXPERTS_TILES;
 }
 
 }  // namespace
@@ -1159,7 +1189,7 @@ int more_experts(const void* X, const void* W1, const void* W2, const int32_t* i
     if (misaligned(X, 16) || misaligned(W1, 16) || misaligned(W2, 16) || misaligned(idx, 4) || misaligned(offsets, 4) ||
         misaligned(sorted_pairs, 4) || misaligned(out_y, 16) || misaligned(out_hidden, 16) || misaligned(workspace, 256))
         return MORE_ERR_ALIGN;
-    const bool pairwise = path == MORE_EXPERTS_PAIRS || !listed || (path == MORE_EXPERTS_AUTO && !out_hidden && more_experts_path(T, h, s, M, k) == MORE_EXPERTS_PAIRS);
+    const bool pairwise = path == MORE_EXPERTS_PAIRS || !listed || (path == MORE_EXPERTS_AUTO && !out_hidden && cheaper_path(T, h, s, M, k) == MORE_EXPERTS_PAIRS);
     if (!pairwise) {
         if (!workspace) return MORE_ERR_NULL;
         if (workspace_bytes < more_experts_workspace(T, h, s, M, k, 0)) return MORE_ERR_TOO_LARGE;
@@ -1180,9 +1210,7 @@ int more_experts(const void* X, const void* W1, const void* W2, const int32_t* i
 int more_experts_path(int T, int h, int s, int M, int k)
 {
     const int rc = check_sizes(T, h, s, M, k);
-    if (rc != MORE_OK) return rc;
-    const long long P = (long long)T * k;
-    return P <= 1024 && P <= M ? MORE_EXPERTS_PAIRS : MORE_EXPERTS_TILES;
+    return rc == MORE_OK ? cheaper_path(T, h, s, M, k) : rc;
 }
 
 int more_experts_backward(const void* X, const void* W1, const void* W2, const int32_t* idx, const int32_t* offsets,

@@ -8,6 +8,8 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <utility>
+
 #include "more_internal.h"
 
 namespace more {
@@ -360,6 +362,26 @@ __device__ __forceinline__ void tc_mma_buffer_ss(uint32_t d, uint32_t a_lo, uint
 }
 #undef MORE_MMA_STEP_SS
 #undef MORE_MMA_OPEN_SS
+
+// A launch behind another of this library's kernels on the same stream: it may begin before that one has ended, and waits for it with
+// wait_for_previous(), before anything that the other writes or reads is touched.  (Transitive: a kernel that has ended has waited.)
+template <class... Params, class... Args>
+cudaError_t launch_behind(void (*kern)(Params...), int grid, int threads, size_t smem, cudaStream_t st, Args&&... args)
+{
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)grid);
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute at;
+    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &at;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kern, std::forward<Args>(args)...);
+}
+__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void let_next_begin() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
 }  // namespace
 
