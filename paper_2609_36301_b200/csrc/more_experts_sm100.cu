@@ -51,6 +51,25 @@ enum { kUp = 0, kDown = 1, kBackAct = 2, kBackX = 3 };
 
 // Loads as a converged warp issues them: every lane passes the same operands and elect.sync picks the lane that issues.  (The
 // instructions take their operands from uniform registers; behind a branch that one lane takes each costs ~150 clocks to issue.)
+// What passes once (weights, their gradients) leaves the L2 cache first, rows by token, which k experts read at different times, last.
+__device__ __forceinline__ uint64_t passes_once()
+{
+    uint64_t h;
+    asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(h));
+    return h;
+}
+__device__ __forceinline__ uint64_t comes_normally()
+{
+    uint64_t h;
+    asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(h));
+    return h;
+}
+__device__ __forceinline__ uint64_t comes_again()
+{
+    uint64_t h;
+    asm volatile("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(h));
+    return h;
+}
 __device__ __forceinline__ void tma_load_2d_elect(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1)
 {
     asm volatile(
@@ -59,12 +78,12 @@ __device__ __forceinline__ void tma_load_2d_elect(uint32_t dst, const CUtensorMa
         ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1)
         : "memory");
 }
-__device__ __forceinline__ void tma_load_3d_elect(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1, int c2)
+__device__ __forceinline__ void tma_load_3d_elect(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1, int c2, uint64_t hint)
 {
     asm volatile(
         "{\n\t.reg .pred pe;\n\telect.sync _|pe, 0xffffffff;\n\t"
-        "@pe cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];\n\t}"
-        ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(c2)
+        "@pe cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%3, %4, %5}], [%2], %6;\n\t}"
+        ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "l"(hint)
         : "memory");
 }
 __device__ __forceinline__ void expect_elect(uint32_t bar, uint32_t bytes)
@@ -74,27 +93,31 @@ __device__ __forceinline__ void expect_elect(uint32_t bar, uint32_t bytes)
         "@pe mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n\t}" ::"r"(bar), "r"(bytes) : "memory");
 }
 // Up to four gathers of four rows each, 512 bytes of shared memory apart, as many as `count` says.
-__device__ __forceinline__ void tma_gather16(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int count, int4 a, int4 b, int4 c, int4 d)
+__device__ __forceinline__ void tma_gather16(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int count, int4 a, int4 b, int4 c, int4 d,
+                                            uint64_t hint)
 {
     asm volatile(
         "{\n\t.reg .pred pe, p0, p1, p2, p3;\n\t.reg .b32 d1, d2, d3;\n\t"
         "elect.sync _|pe, 0xffffffff;\n\t"
         "setp.gt.and.s32 p0, %4, 0, pe;\n\tsetp.gt.and.s32 p1, %4, 1, pe;\n\tsetp.gt.and.s32 p2, %4, 2, pe;\n\tsetp.gt.and.s32 p3, %4, 3, pe;\n\t"
         "add.u32 d1, %0, 512;\n\tadd.u32 d2, %0, 1024;\n\tadd.u32 d3, %0, 1536;\n\t"
-        "@p0 cp.async.bulk.tensor.2d.shared::cta.global.tile::gather4.mbarrier::complete_tx::bytes [%0], [%1, {%3, %5, %6, %7, %8}], [%2];\n\t"
-        "@p1 cp.async.bulk.tensor.2d.shared::cta.global.tile::gather4.mbarrier::complete_tx::bytes [d1], [%1, {%3, %9, %10, %11, %12}], [%2];\n\t"
-        "@p2 cp.async.bulk.tensor.2d.shared::cta.global.tile::gather4.mbarrier::complete_tx::bytes [d2], [%1, {%3, %13, %14, %15, %16}], [%2];\n\t"
-        "@p3 cp.async.bulk.tensor.2d.shared::cta.global.tile::gather4.mbarrier::complete_tx::bytes [d3], [%1, {%3, %17, %18, %19, %20}], [%2];\n\t}"
+        "@p0 cp.async.bulk.tensor.2d.shared::cta.global.tile::gather4.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%3, %5, %6, %7, %8}], [%2], %21;\n\t"
+        "@p1 cp.async.bulk.tensor.2d.shared::cta.global.tile::gather4.mbarrier::complete_tx::bytes.L2::cache_hint [d1], [%1, {%3, %9, %10, %11, %12}], [%2], %21;\n\t"
+        "@p2 cp.async.bulk.tensor.2d.shared::cta.global.tile::gather4.mbarrier::complete_tx::bytes.L2::cache_hint [d2], [%1, {%3, %13, %14, %15, %16}], [%2], %21;\n\t"
+        "@p3 cp.async.bulk.tensor.2d.shared::cta.global.tile::gather4.mbarrier::complete_tx::bytes.L2::cache_hint [d3], [%1, {%3, %17, %18, %19, %20}], [%2], %21;\n\t}"
         ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(count), "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b.x), "r"(b.y), "r"(b.z), "r"(b.w),
-          "r"(c.x), "r"(c.y), "r"(c.z), "r"(c.w), "r"(d.x), "r"(d.y), "r"(d.z), "r"(d.w)
+          "r"(c.x), "r"(c.y), "r"(c.z), "r"(c.w), "r"(d.x), "r"(d.y), "r"(d.z), "r"(d.w), "l"(hint)
         : "memory");
 }
-// Stores that read shared memory by themselves; commit and wait by the thread that issued them.
-__device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, uint32_t src, int c0, int c1, int c2)
+// Stores that read shared memory by themselves; a warp issues, commits and waits for its own.
+__device__ __forceinline__ void tma_store_3d_elect(const CUtensorMap* map, uint32_t src, int c0, int c1, int c2, uint64_t hint)
 {
-    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(map), "r"(src), "r"(c0), "r"(c1),
-                 "r"(c2) : "memory");
+    asm volatile(
+        "{\n\t.reg .pred pe;\n\telect.sync _|pe, 0xffffffff;\n\t"
+        "@pe cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group.L2::cache_hint [%0, {%2, %3, %4}], [%1], %5;\n\t}"
+        ::"l"(map), "r"(src), "r"(c0), "r"(c1), "r"(c2), "l"(hint) : "memory");
 }
+// (every lane, so that it is the issuing one's groups that are meant, whichever that is)
 __device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void bulk_read_done() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory"); }   // all but the last N have read
@@ -139,8 +162,9 @@ struct Ring {
         head = at + bytes;
         return at;
     }
-    // A loader's view of the next stage: true if it is its own and open, at *at.  (*live: false if the CTA is giving up.)
-    __device__ bool open(uint32_t bytes, int loader, int loaders, Control* c, int lane, volatile int* abort_flag, int* status, uint32_t* at, bool* live)
+    // A loader's view of the next stage: true if it is its own.  *at: where it lies; *last: the stage that has to be empty before it is
+    // written, or less than 0.
+    __device__ bool mine(uint32_t bytes, int loader, int loaders, int lane, uint32_t* at, int* last)
     {
         uint32_t from;
         *at = place(bytes, &from);
@@ -149,15 +173,19 @@ struct Ring {
             // Of the last 16 stages those that began more than a ring's length before this one's end have to be empty, and the
             // one whose slot this is (a slot that had none yet counts as one of long ago); they are emptied in order.
             const unsigned old = __ballot_sync(0xffffffffu, lane < kSlots && (lane >= n || lane == n % kSlots || (int)(end - (uint32_t)kXRing - begun) > 0));
-            const int last = n - kSlots + __popc(old) - 1;
-            if (last >= 0 && !mbar_wait(smem_u32(&c->empty[last % kSlots]), (last / kSlots) & 1, abort_flag, status)) {
-                *live = false;
-                return false;
-            }
-            __syncwarp();
+            *last = n - kSlots + __popc(old) - 1;
         }
         if (lane == n % kSlots) begun = from;
         return own;
+    }
+    // The same, and waits until it may be written.  (*live: false if the CTA is giving up.)
+    __device__ bool open(uint32_t bytes, int loader, int loaders, Control* c, int lane, volatile int* abort_flag, int* status, uint32_t* at, bool* live)
+    {
+        int last;
+        if (!mine(bytes, loader, loaders, lane, at, &last)) return false;
+        if (last >= 0 && !mbar_wait(smem_u32(&c->empty[last % kSlots]), (last / kSlots) & 1, abort_flag, status)) *live = false;
+        __syncwarp();
+        return *live;
     }
     __device__ int slot() const { return n % kSlots; }
     __device__ uint32_t parity() const { return (uint32_t)(n / kSlots) & 1u; }
@@ -324,6 +352,7 @@ struct RowsParams {
     int nb;                       // boxes of 64 weight columns per unit
     int chunks;                   // units per tile
     int ksteps;                   // of 64
+    int weights_once;             // most experts have a tile or two
     __nv_bfloat16* out;           // kUp: activation [P][s]; kDown: Y [P][h]
     __nv_bfloat16* hidden;        // kUp: nullable; kBackAct: read
     const float* gate;            // kBackAct
@@ -336,61 +365,63 @@ struct RowsParams {
     int* status;
 };
 
-// The tiles of a CTA's units in turn, and the pairs in N places r, r + 32, ... of each: a unit's pairs are requested a unit ahead, its
-// tile two.
+// The tiles of a CTA's units in turn, and the pairs in N places r, r + 32, ... of each, for a converged warp.  A warp's lanes hold the
+// tiles of 32 units, the next 32 are requested when they begin; pairs are requested a unit ahead.  (What a unit is came from memory
+// once per unit before, a wait of 400 to 1000 clocks for each warp: what the ring leaves of the L1 cache is next to nothing.)
 template <int N>
 struct TilesAhead {
     const RowsParams& p;
-    int units, r, next_pair[N];
-    int step_tile, step_chunk, at_tile, at_chunk;            // units between a CTA's, as tiles and chunks; those of the unit after the next
-    int4 next_tile, last_tile;
-    int unit, chunk, next_chunk, pair[N];
+    int units, r, lane, index, ahead;
+    int4 batch, next_batch;                                  // this lane's: expert, first place, places, chunk
+    int4 coming;                                             // the unit after the present one
+    int next_pair[N];
+    int chunk, pair[N];
     int4 tile;
-    __device__ TilesAhead(const RowsParams& q, int n, int row) : p(q), units(n), r(row), unit((int)blockIdx.x - (int)gridDim.x)
+    __device__ TilesAhead(const RowsParams& q, int n, int row) : p(q), units(n), r(row), lane(threadIdx.x & 31), index(-1), ahead(0)
     {
-        step_tile = (int)gridDim.x / p.chunks;
-        step_chunk = (int)gridDim.x % p.chunks;
-        at_tile = (int)blockIdx.x / p.chunks;
-        at_chunk = (int)blockIdx.x % p.chunks;
-        next_chunk = chunk = at_chunk;
-        next_tile = last_tile = make_int4(0, 0, 0, 0);
-        if ((int)blockIdx.x < units) next_tile = p.tiles[1 + at_tile];
-        advance();
-        if ((int)(blockIdx.x + gridDim.x) < units) last_tile = p.tiles[1 + at_tile];
+        next_batch = request(0);
+        turn();
+        coming = of(0);
         ask_pairs();
         next();
     }
-    __device__ void advance()
+    __device__ int4 request(int first)                       // of units first ... first + 31 of this CTA
     {
-        at_tile += step_tile;
-        at_chunk += step_chunk;
-        if (at_chunk >= p.chunks) {
-            at_chunk -= p.chunks;
-            ++at_tile;
-        }
+        const long long u = blockIdx.x + (long long)(first + lane) * gridDim.x;
+        if (u >= units) return make_int4(0, 0, 0, 0);
+        int4 t = p.tiles[1 + (int)((unsigned)u / (unsigned)p.chunks)];
+        t.w = (int)((unsigned)u % (unsigned)p.chunks);
+        return t;
+    }
+    __device__ void turn()
+    {
+        batch = make_int4(hold(next_batch.x), hold(next_batch.y), hold(next_batch.z), hold(next_batch.w));
+        next_batch = request(ahead + 32);
+    }
+    __device__ int4 of(int i) const
+    {
+        return make_int4(__shfl_sync(0xffffffffu, batch.x, i), __shfl_sync(0xffffffffu, batch.y, i), __shfl_sync(0xffffffffu, batch.z, i),
+                         __shfl_sync(0xffffffffu, batch.w, i));
     }
     __device__ void ask_pairs()
     {
 #pragma unroll
-        for (int i = 0; i < N; ++i) next_pair[i] = r + 32 * i < next_tile.z ? p.pairs[next_tile.y + r + 32 * i] : -1;
+        for (int i = 0; i < N; ++i) next_pair[i] = r + 32 * i < coming.z ? p.pairs[coming.y + r + 32 * i] : -1;
     }
-    __device__ bool more() const { return unit < units; }
+    __device__ bool more() const { return (long long)blockIdx.x + (long long)index * gridDim.x < units; }
     __device__ void next()
     {
-        unit += gridDim.x;
-        chunk = next_chunk;
-        next_chunk = at_chunk;
-        tile = make_int4(hold(next_tile.x), hold(next_tile.y), hold(next_tile.z), 0);
+        ++index;
+        tile = coming;
+        chunk = coming.w;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             pair[i] = hold(next_pair[i]);
             if (pair[i] >= p.P) pair[i] = -1;
         }
-        next_tile = make_int4(hold(last_tile.x), hold(last_tile.y), hold(last_tile.z), 0);
+        if ((++ahead & 31) == 0) turn();
+        coming = of(ahead & 31);
         if constexpr (N > 0) ask_pairs();
-        last_tile = make_int4(0, 0, 0, 0);
-        advance();
-        if (unit < units - 2 * (int)gridDim.x) last_tile = p.tiles[1 + at_tile];
     }
 };
 
@@ -423,6 +454,7 @@ rows_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUte
         constexpr int kMine = kGather ? kLoaders : kFewLoaders;
         const int loader = loader_of(warp);
         int4* rows = ctl->rows[loader];
+        const uint64_t again = comes_again(), once = p.weights_once ? passes_once() : comes_normally();
         Ring rg;
         bool live = true;
         for (TilesAhead<kGather ? 4 : 0> u(p, units, lane); u.more() && live; u.next()) {
@@ -444,14 +476,14 @@ rows_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUte
                     for (int b = 0; b < p.nb; ++b) {
                         const int half = p.nb / 2;
                         const int x = MODE == kDown ? (u.chunk * p.nb + b) * 64 : (b < half ? 0 : p.s) + (u.chunk * half + (b < half ? b : b - half)) * 64;
-                        tma_load_3d_elect(at + a_bytes + b * kBox, &mw, full, x, ks * 64, u.tile.x);
+                        tma_load_3d_elect(at + a_bytes + b * kBox, &mw, full, x, ks * 64, u.tile.x, once);
                     }
                 } else {
-                    tma_load_3d_elect(at + a_bytes, &mw, full, ks * 64, u.chunk * p.nb * 64, u.tile.x);
+                    tma_load_3d_elect(at + a_bytes, &mw, full, ks * 64, u.chunk * p.nb * 64, u.tile.x, once);
                 }
                 if constexpr (kGather) {
                     for (int g = 0; g < gathers; g += 4)
-                        tma_gather16(at + g * 512, &ma, full, ks * 64, gathers - g, rows[g], rows[g + 1], rows[g + 2], rows[g + 3]);
+                        tma_gather16(at + g * 512, &ma, full, ks * 64, gathers - g, rows[g], rows[g + 1], rows[g + 2], rows[g + 3], again);
                 } else {
                     for (int b = 0; b < 4; ++b) tma_load_2d_elect(at + b * 4096, &ma, full, ks * 64, u.tile.y + (b & (unlike - 1)) * 32);
                 }
@@ -706,44 +738,57 @@ struct WeightsParams {
     Divide by_k;
     int a_by_token;               // dW1: A = X by token, B = du by place; dW2: A = gate a by place, B = d by token
     int rows, cols;               // of an expert's output: A's columns, B's columns
-    int mtiles, chunks, nb;
+    int mtiles, chunks, nb, box_rows;
+    // Boxes of 64 of A's columns, rows of the accumulator.  Where the output has no more than 64 rows they are loaded twice: both halves
+    // of the accumulator's lanes then hold the same, and all the warps that read it share the columns.
+    __device__ int boxes_of_rows(int mt) const { return rows <= 64 || rows - mt * 128 > 64 ? 2 : 1; }
+    __device__ bool twice() const { return rows <= 64; }
     __nv_bfloat16* out;           // [M][rows][cols]
     int* status;
 };
 
-// The runs of a CTA's units in turn, the next one's bounds requested while the present one is worked on.
+// The runs of a CTA's units in turn, for a converged warp, whose lanes hold those of 32 units; the next 32 are requested when they begin.
 struct Units {
     const WeightsParams& p;
-    uint32_t per_expert, units, unit;
-    int e, rem;                   // of the present unit: expert, which of the expert's units
-    int lo, n;                    // its run
-    int next_e, next_rem, raw_lo, raw_hi;
-    __device__ explicit Units(const WeightsParams& q) : p(q), per_expert(q.mtiles * q.chunks), units((uint32_t)q.M * per_expert), unit(blockIdx.x)
+    uint32_t per_expert, units;
+    int lane, index;
+    int e, mt, chunk, lo, n;                                 // of the present unit: expert, tile of rows, chunk of columns, its run
+    int batch_e, batch_rem, raw_lo, raw_hi;                  // this lane's
+    int next_e, next_rem, next_lo, next_hi;
+    __device__ explicit Units(const WeightsParams& q) : p(q), per_expert(q.mtiles * q.chunks), units((uint32_t)q.M * per_expert),
+                                                        lane(threadIdx.x & 31), index(-1)
     {
-        next_e = next_rem = raw_lo = raw_hi = 0;
-        request();
+        request(0);
         next();
     }
-    __device__ void request()                               // (of the unit that `unit` names)
+    __device__ void request(int first)
     {
-        if (unit >= units) return;
-        next_e = (int)(unit / per_expert);
-        next_rem = (int)(unit - (uint32_t)next_e * per_expert);
-        raw_lo = p.offsets[next_e];
-        raw_hi = p.offsets[next_e + 1];
+        const unsigned long long u = blockIdx.x + (unsigned long long)(first + lane) * gridDim.x;
+        next_e = next_rem = next_lo = next_hi = 0;
+        if (u >= units) return;
+        next_e = (int)((uint32_t)u / per_expert);
+        next_rem = (int)((uint32_t)u % per_expert);
+        next_lo = p.offsets[next_e];
+        next_hi = p.offsets[next_e + 1];
     }
-    __device__ bool more() const { return unit - gridDim.x < units; }
-    __device__ void next()                                  // (whatever the offsets hold, a run stays within the places)
+    __device__ bool more() const { return blockIdx.x + (unsigned long long)index * gridDim.x < units; }
+    __device__ void next()
     {
-        e = next_e;
-        rem = next_rem;
-        lo = min(max(hold(raw_lo), 0), p.P);
-        n = max(min(hold(raw_hi), p.P) - lo, 0);
-        unit += gridDim.x;
-        request();
+        const int i = ++index & 31;
+        if (i == 0) {
+            batch_e = hold(next_e);
+            batch_rem = hold(next_rem);
+            raw_lo = min(max(hold(next_lo), 0), p.P);        // (whatever the offsets hold, a run stays within the places)
+            raw_hi = max(min(hold(next_hi), p.P), raw_lo);
+            request(index + 32);
+        }
+        e = __shfl_sync(0xffffffffu, batch_e, i);
+        const int rem = __shfl_sync(0xffffffffu, batch_rem, i);
+        mt = p.chunks == 1 ? rem : rem / p.chunks;
+        chunk = p.chunks == 1 ? 0 : rem % p.chunks;
+        lo = __shfl_sync(0xffffffffu, raw_lo, i);
+        n = __shfl_sync(0xffffffffu, raw_hi, i) - lo;
     }
-    __device__ int mtile() const { return p.chunks == 1 ? rem : rem / p.chunks; }
-    __device__ int chunk() const { return p.chunks == 1 ? 0 : rem % p.chunks; }
 };
 
 __global__ void __launch_bounds__(threads_of(kLoaders), 1)
@@ -764,48 +809,76 @@ weights_kernel(const __grid_constant__ CUtensorMap mtoken, const __grid_constant
         // A stage is up to 64 rows, as many whole MMA steps of 16 as it needs, of both operands' boxes of 64 columns: rows by token by
         // gathers, consecutive places in pieces of 16.  Rows behind the run's last are out of bounds, zeros: of the places, too,
         // only then row by row (what lies there belongs to another expert).
+        // A loader issues a stage of its own when it has come to the next one, whose pairs it has just requested.
         const int loader = loader_of(warp);
         int4* rows = ctl->rows[loader];                             // 64 tokens, 64 places
+        const uint64_t again = comes_again();
         Ring rg;
         bool live = true;
-        for (Units u(p); u.more() && live; u.next()) {
-            const int mt = u.mtile(), chunk = u.chunk(), a_boxes = p.rows - mt * 128 > 64 ? 2 : 1;
-            for (int at = 0; at < u.n && live; at += 64, ++rg.n) {
-                const int left = min(64, u.n - at), steps = (left + 15) / 16;
-                const uint32_t box = (uint32_t)steps * 2048;
-                uint32_t where;
-                const uint32_t bytes = box * (a_boxes + p.nb);
-                if (rg.n % kLoaders == loader) {
+        struct Own {
+            int first, left, mt, chunk, last, slot, pair[2];        // first place, rows; the stage that has to be empty, or less than 0
+            uint32_t where;
+        } own;
+        own.left = 0;
+        auto issue = [&]() {
+            if (own.left == 0 || !live) return;
+            const int left = own.left, steps = (left + 15) / 16, a_boxes = p.boxes_of_rows(own.mt);
+            const uint32_t box = (uint32_t)steps * 2048;
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const int r = i * 32 + lane, place = u.lo + at + r, pair = r < left ? p.pairs[place] : -1;
-                        const bool in = pair >= 0 && pair < p.P;
-                        reinterpret_cast<int*>(rows)[r] = in ? p.by_k(pair) : p.T;
-                        reinterpret_cast<int*>(rows)[64 + r] = in ? place : p.P;
-                    }
-                    __syncwarp();
+            for (int i = 0; i < 2; ++i) {
+                const int r = i * 32 + lane, pair = hold(own.pair[i]);
+                const bool in = pair >= 0 && pair < p.P;
+                reinterpret_cast<int*>(rows)[r] = in ? p.by_k(pair) : p.T;
+                reinterpret_cast<int*>(rows)[64 + r] = in ? own.first + r : p.P;
+            }
+            if (own.last >= 0 && !mbar_wait(smem_u32(&ctl->empty[own.last % kSlots]), (own.last / kSlots) & 1, abort_flag, p.status)) {
+                live = false;
+                return;
+            }
+            __syncwarp();
+            const uint32_t full = smem_u32(&ctl->full[own.slot]);
+            expect_elect(full, box * (a_boxes + p.nb));
+            const uint32_t a_at = ring + own.where, b_at = a_at + a_boxes * box;
+            const int a_x = own.mt * 128, b_x = own.chunk * p.nb * 64;
+            const int t_boxes = p.a_by_token ? a_boxes : p.nb, p_boxes = p.a_by_token ? p.nb : a_boxes;
+            const int t_x = p.a_by_token ? a_x : b_x, p_x = p.a_by_token ? b_x : a_x;
+            const int t_step = p.a_by_token && p.twice() ? 0 : 64, p_step = !p.a_by_token && p.twice() ? 0 : 64;
+            const uint32_t t_at = p.a_by_token ? a_at : b_at, p_at = p.a_by_token ? b_at : a_at;
+            for (int q = 0; q < steps; ++q) {
+                const int4 r0 = rows[4 * q], r1 = rows[4 * q + 1], r2 = rows[4 * q + 2], r3 = rows[4 * q + 3];
+                for (int b = 0; b < t_boxes; ++b) tma_gather16(t_at + b * box + q * 2048, &mtoken, full, t_x + b * t_step, 4, r0, r1, r2, r3, again);
+                if (left >= q * 16 + 16) {
+                    for (int b = 0; b < p_boxes; ++b) tma_load_2d_elect(p_at + b * box + q * 2048, &mplace16, full, p_x + b * p_step, own.first + q * 16);
+                } else {
+                    const int4 s0 = rows[16 + 4 * q], s1 = rows[17 + 4 * q], s2 = rows[18 + 4 * q], s3 = rows[19 + 4 * q];
+                    for (int b = 0; b < p_boxes; ++b) tma_gather16(p_at + b * box + q * 2048, &mplace, full, p_x + b * p_step, 4, s0, s1, s2, s3, again);
                 }
-                if (!rg.open(bytes, loader, kLoaders, ctl, lane, abort_flag, p.status, &where, &live)) continue;
-                const uint32_t full = smem_u32(&ctl->full[rg.slot()]);
-                expect_elect(full, bytes);
-                const uint32_t a_at = ring + where, b_at = a_at + a_boxes * box;
-                const int a_x = mt * 128, b_x = chunk * p.nb * 64;
-                const int t_boxes = p.a_by_token ? a_boxes : p.nb, p_boxes = p.a_by_token ? p.nb : a_boxes;
-                const int t_x = p.a_by_token ? a_x : b_x, p_x = p.a_by_token ? b_x : a_x;
-                const uint32_t t_at = p.a_by_token ? a_at : b_at, p_at = p.a_by_token ? b_at : a_at;
-                for (int q = 0; q < steps; ++q) {
-                    const int4 r0 = rows[4 * q], r1 = rows[4 * q + 1], r2 = rows[4 * q + 2], r3 = rows[4 * q + 3];
-                    for (int b = 0; b < t_boxes; ++b) tma_gather16(t_at + b * box + q * 2048, &mtoken, full, t_x + b * 64, 4, r0, r1, r2, r3);
-                    if (left >= q * 16 + 16) {
-                        for (int b = 0; b < p_boxes; ++b) tma_load_2d_elect(p_at + b * box + q * 2048, &mplace16, full, p_x + b * 64, u.lo + at + q * 16);
-                    } else {
-                        const int4 s0 = rows[16 + 4 * q], s1 = rows[17 + 4 * q], s2 = rows[18 + 4 * q], s3 = rows[19 + 4 * q];
-                        for (int b = 0; b < p_boxes; ++b) tma_gather16(p_at + b * box + q * 2048, &mplace, full, p_x + b * 64, 4, s0, s1, s2, s3);
-                    }
-                }
-                __syncwarp();                                       // (the rows are read)
+            }
+            __syncwarp();                                           // (the rows are read)
+        };
+        for (Units u(p); u.more() && live; u.next()) {
+            const int a_boxes = p.boxes_of_rows(u.mt);
+            for (int at = 0; at < u.n; at += 64, ++rg.n) {
+                const int left = min(64, u.n - at);
+                uint32_t where;
+                int last;
+                if (!rg.mine((uint32_t)((left + 15) / 16) * 2048 * (a_boxes + p.nb), loader, kLoaders, lane, &where, &last)) continue;
+                int pair[2];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) pair[i] = i * 32 + lane < left ? p.pairs[u.lo + at + i * 32 + lane] : -1;
+                issue();
+                own.first = u.lo + at;
+                own.left = left;
+                own.mt = u.mt;
+                own.chunk = u.chunk;
+                own.last = last;
+                own.slot = rg.slot();
+                own.where = where;
+                own.pair[0] = pair[0];
+                own.pair[1] = pair[1];
             }
         }
+        issue();
     } else if (warp == 1) {
         const uint32_t idesc = idesc_of(p.nb * 64, 1, 1);
         const uint64_t d0 = umma_desc_sw128(ring, 0, 1024);
@@ -815,7 +888,7 @@ weights_kernel(const __grid_constant__ CUtensorMap mtoken, const __grid_constant
         for (Units u(p); u.more() && live; u.next()) {
             const int n = u.n;
             if (n == 0) continue;                                   // (the epilogue writes zeros without an accumulator)
-            const int buf = it & 1, a_boxes = p.rows - u.mtile() * 128 > 64 ? 2 : 1;
+            const int buf = it & 1, a_boxes = p.boxes_of_rows(u.mt);
             if (!mbar_wait(smem_u32(&ctl->acc_empty[buf]), ((it >> 1) & 1) ^ 1u, abort_flag, p.status)) break;
             tc_fence_after();
             for (int at = 0; at < n; at += 64) {
@@ -835,13 +908,15 @@ weights_kernel(const __grid_constant__ CUtensorMap mtoken, const __grid_constant
             ++it;
         }
     } else {
-        // bf16 boxes of 128 rows x 64 columns in the layout of a swizzled TMA store, which cuts off what is behind the ends; as many
-        // units' worth of them as staging holds
-        const int quarter = warp & 3, side = warp >= 6, row = quarter * 32 + lane, tid = threadIdx.x - 64;
-        const int buffers = p.nb == 4 ? 1 : 2;
+        // bf16 boxes of 64 columns in the layout of a swizzled TMA store, which cuts off what is behind the ends, of 128 rows, or of 64
+        // where no more are needed; two units' worth of them where staging holds that
+        const int quarter = warp & 3, side = warp >= 6, tid = threadIdx.x - 64;
+        const int copies = p.twice() ? 2 : 1, copy = p.twice() ? quarter >> 1 : 0, row0 = (p.twice() ? quarter & 1 : quarter) * 32, row = row0 + lane;
+        const uint64_t once = passes_once();
+        const int box = p.box_rows * 128, buffers = 2 * p.nb * box <= kXStaging ? 2 : 1;
         int it = 0;
         for (Units w(p); w.more(); w.next()) {
-            const int mt = w.mtile(), per = p.nb * 32, c0 = w.chunk() * p.nb * 64;
+            const int mt = w.mt, per = p.nb * 32, c0 = w.chunk * p.nb * 64;
             const int rows = min(128, p.rows - mt * 128);
             if (w.n == 0) {                                         // zeros: threads along rows, 16 bytes each
                 const int pieces = p.nb * 8, c = c0 + (tid & (pieces - 1)) * 8;
@@ -852,12 +927,12 @@ weights_kernel(const __grid_constant__ CUtensorMap mtoken, const __grid_constant
                 continue;
             }
             const int buf = it & 1;
-            const uint32_t acc = tmem + buf * 256 + ((uint32_t)(quarter * 32) << 16), to = staging + (it & (buffers - 1)) * (2 * 16384);
+            const uint32_t acc = tmem + buf * 256 + ((uint32_t)(quarter * 32) << 16), to = staging + (it & (buffers - 1)) * p.nb * box;
             const bool ok = mbar_wait(smem_u32(&ctl->acc_full[buf]), (it >> 1) & 1, abort_flag, p.status);   // (given up: goes on without work)
             tc_fence_after();
-            if (tid == 0) buffers == 2 ? bulk_read_done<1>() : bulk_read_done<0>();
+            if (warp == 2) buffers == 2 ? bulk_read_done<1>() : bulk_read_done<0>();
             epilogue_sync();
-            for (int c = 0; ok && c < per && quarter * 32 < rows && c0 + side * per + c < p.cols; c += 32) {
+            for (int c = copy * 32; ok && c < per && row0 < rows && c0 + side * per + c < p.cols; c += copies * 32) {
                 float v[2][16];
 #pragma unroll
                 for (int i = 0; i < 2; ++i) tmem_ld16(acc + side * per + c + i * 16, v[i]);
@@ -865,8 +940,8 @@ weights_kernel(const __grid_constant__ CUtensorMap mtoken, const __grid_constant
                 for (int i = 0; i < 2; ++i) {
                     tmem_ld_wait16(v[i]);
                     const int col = side * per + c + i * 16;
-                    st_piece(staged(to + col / 64 * 16384, 128, row, col % 64 / 8), pack8(v[i], 0));
-                    st_piece(staged(to + col / 64 * 16384, 128, row, col % 64 / 8 + 1), pack8(v[i], 8));
+                    st_piece(staged(to + col / 64 * box, 128, row, col % 64 / 8), pack8(v[i], 0));
+                    st_piece(staged(to + col / 64 * box, 128, row, col % 64 / 8 + 1), pack8(v[i], 8));
                 }
             }
             tc_fence_before();
@@ -874,12 +949,12 @@ weights_kernel(const __grid_constant__ CUtensorMap mtoken, const __grid_constant
             ++it;
             fence_async_smem();
             epilogue_sync();
-            if (tid == 0) {
-                for (int b = 0; ok && b < p.nb && c0 + b * 64 < p.cols; ++b) tma_store_3d(&mout, to + b * 16384, c0 + b * 64, mt * 128, w.e);
+            if (warp == 2) {
+                for (int b = 0; ok && b < p.nb && c0 + b * 64 < p.cols; ++b) tma_store_3d_elect(&mout, to + b * box, c0 + b * 64, mt * 128, w.e, once);
                 bulk_commit();
             }
         }
-        if (tid == 0) bulk_all_done();
+        if (warp == 2) bulk_all_done();
     }
     close_cta(ctl, tmem, warp);
 }
@@ -900,30 +975,37 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ JoinP
 {
     let_next_begin();
     wait_for_previous();
-    const int vecs = p.h / 8;
-    const long long all = p.out_dx ? (long long)p.T * vecs : 0;
-    const long long first = (long long)blockIdx.x * 256 + threadIdx.x, stride = (long long)gridDim.x * 256;
-    for (long long i = first; i < all; i += stride) {
-        const int t = (int)(i / vecs), c = (int)(i % vecs) * 8;
+    const int vecs = p.h / 8, width = vecs < 256 ? vecs : 256, tokens = 256 / width;      // threads of a token, tokens of a CTA
+    const int mine = threadIdx.x / width, first_vec = threadIdx.x % width;
+    for (long long t = p.out_dx && mine < tokens ? (long long)blockIdx.x * tokens + mine : p.T; t < p.T; t += (long long)gridDim.x * tokens)
+    for (int c = first_vec * 8; c < p.h; c += width * 8) {
         float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        for (int j = 0; j < p.k; ++j) {
-            const long long pair = (long long)t * p.k + j;
-            if ((unsigned)p.idx[pair] >= (unsigned)p.M) continue;
-            const float sc = __int_as_float((int)p.dx_scale[pair * p.dx_groups + c / 32] << 23);
-            const uint4 u = *reinterpret_cast<const uint4*>(p.dx + pair * p.h + c);
-            const __half2* q = reinterpret_cast<const __half2*>(&u);
+        for (int j0 = 0; j0 < p.k; j0 += 4) {                // four slots' loads at a time
+            uint4 u[4];
+            float sc[4];
 #pragma unroll
-            for (int a = 0; a < 4; ++a) {
-                const float2 f = __half22float2(q[a]);
-                v[2 * a] = fmaf(f.x, sc, v[2 * a]);
-                v[2 * a + 1] = fmaf(f.y, sc, v[2 * a + 1]);
+            for (int j = 0; j < 4; ++j) {
+                const long long pair = t * p.k + j0 + j;
+                const bool in = j0 + j < p.k && (unsigned)p.idx[pair] < (unsigned)p.M;
+                sc[j] = in ? __int_as_float((int)p.dx_scale[pair * p.dx_groups + c / 32] << 23) : 0.f;
+                u[j] = in ? *reinterpret_cast<const uint4*>(p.dx + pair * p.h + c) : make_uint4(0, 0, 0, 0);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const __half2* q = reinterpret_cast<const __half2*>(&u[j]);
+#pragma unroll
+                for (int a = 0; a < 4; ++a) {
+                    const float2 f = __half22float2(q[a]);
+                    v[2 * a] = fmaf(f.x, sc[j], v[2 * a]);
+                    v[2 * a + 1] = fmaf(f.y, sc[j], v[2 * a + 1]);
+                }
             }
         }
-        *reinterpret_cast<uint4*>(p.out_dx + (long long)t * p.h + c) =
+        *reinterpret_cast<uint4*>(p.out_dx + t * p.h + c) =
             make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
     }
     if (!p.out_dgate) return;
-    for (long long i = first; i < p.P; i += stride) {
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < p.P; i += (long long)gridDim.x * 256) {
         float sum = 0.f;
         if ((unsigned)p.idx[i] < (unsigned)p.M)
             for (int q = 0; q < p.parts; ++q) sum += p.dgate_part[(long long)q * p.P + i];
@@ -1014,7 +1096,8 @@ int launch_tiles(const ExpertsArgs& a, cudaStream_t st)
 int launch_weights(const CUtensorMap& mtoken, const CUtensorMap (&mplace)[2], WeightsParams p, const DeviceCtx& ctx, cudaStream_t st)
 {
     CUtensorMap mout;
-    const int rc = weight_map(p.out, p.M, p.rows, p.cols, 128, &mout);
+    p.box_rows = p.rows > 64 ? 128 : 64;
+    const int rc = weight_map(p.out, p.M, p.rows, p.cols, p.box_rows, &mout);
     if (rc != MORE_OK) return rc;
     if (allow_smem(weights_kernel) != MORE_OK) return MORE_ERR_CUDA;
     p.nb = p.cols > 128 ? 4 : (p.cols > 64 ? 2 : 1);
@@ -1049,6 +1132,7 @@ int launch_experts(const ExpertsArgs& a, const DeviceCtx& ctx)
     const long long tiles = tile_capacity(a.T, a.M, a.k);
     p.by_k.by(a.k);
     p.rows = a.T;
+    p.weights_once = P <= 2LL * kTileRows * a.M;
     p.nb = a.s > 64 ? 4 : 2;
     p.chunks = (a.s + p.nb * 32 - 1) / (p.nb * 32);
     p.ksteps = (a.h + 63) / 64;
@@ -1085,6 +1169,7 @@ int launch_experts_backward(const ExpertsArgs& a, const DeviceCtx& ctx)
     p.P = (int)P; p.h = a.h; p.s = a.s;
     p.by_k.by(a.k);
     p.rows = a.T;
+    p.weights_once = P <= 2LL * kTileRows * a.M;
     p.nb = back_boxes(a.s);
     p.chunks = (a.s + p.nb * 64 - 1) / (p.nb * 64);
     p.ksteps = (a.h + 63) / 64;
@@ -1100,6 +1185,7 @@ int launch_experts_backward(const ExpertsArgs& a, const DeviceCtx& ctx)
     p.dx = reinterpret_cast<__half*>(base + w.dx);
     p.dx_scale = reinterpret_cast<uint8_t*>(base + w.dx_scale);
     if (a.out_dx) {
+        p.weights_once = 0;                                          // (a row of W1 is read in pieces, a step apart)
         p.nb = row_boxes(a.h);
         p.chunks = (a.h + p.nb * 64 - 1) / (p.nb * 64);
         p.ksteps = (2 * a.s + 63) / 64;
