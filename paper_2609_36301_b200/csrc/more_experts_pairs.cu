@@ -18,7 +18,7 @@ __device__ __forceinline__ float ld_cluster(uint32_t addr, int rank)
     uint32_t remote;
     float v;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(addr), "r"(rank));
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(remote) : "memory");
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(remote));
     return v;
 }
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
@@ -74,9 +74,12 @@ struct Slice {
 // red[row group][8 columns of a group] -> the sum of column c of `cols`
 __device__ __forceinline__ float column_sum(const float* red, int cols, int row_groups, int c)
 {
-    float v = 0.f;
-    for (int r = 0; r < row_groups; ++r) v += red[r * cols + c];
-    return v;
+    float v[4] = {0.f, 0.f, 0.f, 0.f};                 // (four chains, so that their loads do not wait for one another)
+    for (int r = 0; r < row_groups; r += 4)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (r + i < row_groups) v[i] += red[(r + i) * cols + c];
+    return (v[0] + v[1]) + (v[2] + v[3]);
 }
 
 // BATCH, PER_SM: what a CTA has in flight, and how many of them are resident.
@@ -131,10 +134,16 @@ pairs_kernel(const __nv_bfloat16* __restrict__ X, const __nv_bfloat16* __restric
     cluster_wait();
     const uint32_t part_at = smem_u32(part);
     for (int c = tid; c < s; c += kPThreads) {
-        float g = 0.f, u = 0.f;
-        for (int q = 0; q < ranks; ++q) {
-            g += ld_cluster(part_at + c * 4, q);
-            u += ld_cluster(part_at + (s + c) * 4, q);
+        float gq[8], uq[8], g = 0.f, u = 0.f;              // (at most 8 CTAs; all their parts requested at once)
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+            gq[q] = q < ranks ? ld_cluster(part_at + c * 4, q) : 0.f;
+            uq[q] = q < ranks ? ld_cluster(part_at + (s + c) * 4, q) : 0.f;
+        }
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+            g += gq[q];
+            u += uq[q];
         }
         act[c] = g * sigmoidf(g) * u;
     }

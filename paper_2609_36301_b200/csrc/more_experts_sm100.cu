@@ -218,11 +218,9 @@ __global__ void __launch_bounds__(1024) tiles_kernel(const int32_t* __restrict__
     if (lane == 31) warp_sum[warp] = incl;
     if (lane == 0) warp_before[warp] = before;
     __syncthreads();
-    int at = incl - mine;
-    for (int w = 0; w < 32; ++w) {
-        at += warp_before[w];
-        if (w < warp) at += warp_sum[w];
-    }
+    int others = warp_before[lane] + (lane < warp ? warp_sum[lane] : 0);
+    for (int o = 16; o > 0; o >>= 1) others += __shfl_xor_sync(0xffffffffu, others, o);
+    const int at = others + incl - mine;
     for (int i = 0; i < mine && at + i < capacity; ++i)
         tiles[1 + at + i] = make_int4(e, lo + i * kTileRows, min(kTileRows, n - i * kTileRows), 0);
     if (e == M - 1) tiles[0].x = min(at + mine, capacity);
