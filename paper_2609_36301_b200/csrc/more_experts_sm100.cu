@@ -41,11 +41,15 @@ constexpr int kBox = 64 * 128;                       // 64 rows of 64 bf16
 constexpr int kRowPitch = 528;                       // a staged output row: 256 16-bit values, and 16 bytes so that rows fall on other banks
 constexpr int kXStaging = kTileRows * kRowPitch;     // what the epilogue passes from the tensor memory's layout to memory's
 constexpr int kXRing = 154 * 1024;
-constexpr int kXControl = 1024 + kLoaders * 512;
+constexpr int kXControl = 1536 + kLoaders * 512;
 constexpr int kXSmem = kXRing + kXStaging + 1024 /*alignment*/ + kXControl;
 static_assert(kXSmem <= 227 * 1024, "shared memory");
 static_assert(kXStaging >= kTileRows * 128, "an operand of fewer rows than the MMA's 128 is read past its end");
 constexpr int kSlots = 16;                           // stages in flight at most
+// kBackAct adds up this many steps (512 columns) in the tensor memory, whose sums are truncated at every 16 columns, and those sums in
+// rounding registers: the gate gradients, which leave in 32 bits, were 4.6e-6 off relative to their size at h = 4096, 4e-6 of it a
+// bias towards zero, in one piece, and are as good as at h = 512, 4.7e-7, in pieces.
+constexpr int kSumSteps = 8;
 
 enum { kUp = 0, kDown = 1, kBackAct = 2, kBackX = 3 };
 
@@ -141,6 +145,7 @@ struct Control {
     uint32_t tmem;
     int abort;
     int pair[kTileRows];
+    float gate[kTileRows];
     int4 rows[kLoaders][kTileRows / 4];   // of each loader's tile
 };
 static_assert(sizeof(Control) <= kXControl, "control block");
@@ -266,6 +271,14 @@ __device__ __forceinline__ void stage_f32(uint32_t base, int pitch, int row, int
     for (int i = 0; i < 4; ++i)
         st_piece(staged(base, pitch, row, piece + i), make_uint4(__float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]),
                                                                  __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3])));
+}
+__device__ __forceinline__ void add_staged(const uint8_t* base, int pitch, int row, int piece, float (&v)[16])
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float4 a = *reinterpret_cast<const float4*>(base + staged(0, pitch, row, piece + i));
+        v[4 * i] += a.x; v[4 * i + 1] += a.y; v[4 * i + 2] += a.z; v[4 * i + 3] += a.w;
+    }
 }
 __device__ __forceinline__ void unstage8(const uint8_t* base, int pitch, int row, int piece, float (&v)[8])
 {
@@ -496,12 +509,15 @@ rows_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUte
         Ring rg;
         int it = 0;
         bool live = true;
-        for (TilesAhead<0> u(p, units, 0); u.more() && live; u.next(), ++it) {
-            const int buf = it & 1;
+        for (TilesAhead<0> u(p, units, 0); u.more() && live; u.next()) {
             const uint32_t a_bytes = row_bytes<kGather>(u.tile.z), bytes = a_bytes + p.nb * kBox;
-            if (!mbar_wait(smem_u32(&ctl->acc_empty[buf]), ((it >> 1) & 1) ^ 1u, abort_flag, p.status)) break;
-            tc_fence_after();
             for (int ks = 0; ks < p.ksteps; ++ks) {
+                const int in_block = MODE == kBackAct ? ks % kSumSteps : ks;
+                const uint32_t d = tmem + (it & 1) * 256;
+                if (in_block == 0) {
+                    if (!mbar_wait(smem_u32(&ctl->acc_empty[it & 1]), ((it >> 1) & 1) ^ 1u, abort_flag, p.status)) { live = false; break; }
+                    tc_fence_after();
+                }
                 uint32_t from;
                 const uint32_t off = rg.place(bytes, &from);
                 if (!mbar_wait(smem_u32(&ctl->full[rg.slot()]), rg.parity(), abort_flag, p.status)) { live = false; break; }
@@ -509,11 +525,14 @@ rows_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUte
                 const uint32_t al = (uint32_t)a0 + (off >> 4), bl = (uint32_t)b0 + ((off + a_bytes) >> 4);
 #pragma unroll
                 for (int q = 0; q < 4; ++q)
-                    tc_mma_bf16_ss_elect(tmem + buf * 256, al + q * 2, a_hi, bl + q * kBStep, b_hi, idesc, ks > 0 || q > 0);
+                    tc_mma_bf16_ss_elect(d, al + q * 2, a_hi, bl + q * kBStep, b_hi, idesc, in_block > 0 || q > 0);
                 tc_commit_elect(smem_u32(&ctl->empty[rg.slot()]));
                 ++rg.n;
+                if (ks == p.ksteps - 1 || (MODE == kBackAct && in_block == kSumSteps - 1)) {
+                    tc_commit_elect(smem_u32(&ctl->acc_full[it & 1]));
+                    ++it;
+                }
             }
-            if (live) tc_commit_elect(smem_u32(&ctl->acc_full[buf]));
         }
     } else if constexpr (MODE == kUp) {
         // Thread by row: a warp works on 32 rows and half of the columns, and passes what it has to write through staging of its own, so
@@ -558,52 +577,59 @@ rows_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUte
             warp_arrive(smem_u32(&ctl->acc_empty[buf]), lane);
         }
     } else if constexpr (MODE == kBackAct) {
-        // Two steps per pass: the warps that have rows copy columns of the accumulator into staging, thread by row; then all
-        // eight work along rows, so that memory is read and written in whole lines and a tile of few rows occupies them all.
-        const int quarter = warp & 3, side = warp >= 6;             // lane quarter of the accumulator; half of the columns
+        // The warps that have rows add columns of the accumulator up in staging, thread by row; then all eight work along rows, so that
+        // memory is read and written in whole lines and a tile of few rows occupies them all.
+        const int quarter = warp & 3, side = warp >= 6;             // lane quarter of the accumulator; half of every 64 columns
         const int r0 = quarter * 32, row = r0 + lane;               // this warp's first row of a tile, this thread's
-        const int tid = threadIdx.x - 64;
+        const int tid = threadIdx.x - 64, blocks = (p.ksteps + kSumSteps - 1) / kSumSteps;
         int it = 0;
-        for (TilesAhead<1> u(p, units, row); u.more(); u.next(), ++it) {
+        for (TilesAhead<1> u(p, units, row); u.more(); u.next()) {
             const int4 tile = u.tile;
-            const int chunk = u.chunk, buf = it & 1;
-            const uint32_t acc = tmem + buf * 256 + ((uint32_t)r0 << 16);
-            uint4 kept[4][2];                                       // both projections of this thread's first items
+            const int first = u.chunk * p.nb * 64, passes = (min(p.nb * 64, p.s - first) + 63) / 64;      // of 64 columns, at most two
+            // requested before the waits: both projections of this thread's first items, this row's gate
+            uint4 kept[4][2];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int r = (i * 256 + tid) >> 3, col = chunk * p.nb * 64 + (tid & 7) * 8;
+                const int r = (i * 256 + tid) >> 3, col = first + (tid & 7) * 8;
                 if (r < tile.z && col < p.s) {
                     const __nv_bfloat16* from = p.hidden + (long long)(tile.y + r) * 2 * p.s + col;
                     kept[i][0] = *reinterpret_cast<const uint4*>(from);
                     kept[i][1] = *reinterpret_cast<const uint4*>(from + p.s);
                 }
             }
-            // after a wait that gave up the loop goes on without work: no warp is left alone at a barrier
-            const bool ok = mbar_wait(smem_u32(&ctl->acc_full[buf]), (it >> 1) & 1, abort_flag, p.status);
-            tc_fence_after();
-            const int rows = ok ? tile.z : 0;
-            const bool any = r0 < rows;                             // (a warp whose rows are all behind the tile copies nothing)
-            auto release = [&]() {                                  // the accumulator may be filled again
+            const float gate = side == 0 && u.pair[0] >= 0 ? p.gate[u.pair[0]] : 0.f;
+            bool ok = true;
+            for (int block = 0; block < blocks; ++block, ++it) {
+                const int buf = it & 1;
+                const uint32_t acc = tmem + buf * 256 + ((uint32_t)r0 << 16);
+                // after a wait that gave up the loop goes on without work: no warp is left alone at a barrier
+                ok &= mbar_wait(smem_u32(&ctl->acc_full[buf]), (it >> 1) & 1, abort_flag, p.status);
+                tc_fence_after();
+                if (ok && r0 < tile.z)                              // (a warp whose rows are all behind the tile adds nothing)
+                    for (int pass = 0; pass < passes; ++pass) {
+                        float v[2][16];
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) tmem_ld16(acc + pass * 64 + side * 32 + i * 16, v[i]);
+                        const int at = pass * kTileRows * 256;
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            tmem_ld_wait16(v[i]);
+                            if (block > 0) add_staged(staging_at + at, 256, row, side * 8 + i * 4, v[i]);
+                            stage_f32(staging + at, 256, row, side * 8 + i * 4, v[i]);
+                        }
+                    }
                 tc_fence_before();
-                warp_arrive(smem_u32(&ctl->acc_empty[buf]), lane);
-            };
-            const int width = p.nb * 64, passes = (min(width, p.s - chunk * width) + 63) / 64;
-            if (side == 0) ctl->pair[row] = u.pair[0];          // (the last tile's have been read)
+                warp_arrive(smem_u32(&ctl->acc_empty[buf]), lane);  // the accumulator may be filled again
+            }
+            if (side == 0) {                                        // (the last tile's have been read)
+                ctl->pair[row] = u.pair[0];
+                ctl->gate[row] = gate;
+            }
+            epilogue_sync();
+            const int rows = ok ? tile.z : 0;
             float dg[4] = {0.f, 0.f, 0.f, 0.f};
             for (int pass = 0; pass < passes; ++pass) {
-                if (any) {
-                    float v[2][16];
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) tmem_ld16(acc + pass * 64 + side * 32 + i * 16, v[i]);
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        tmem_ld_wait16(v[i]);
-                        stage_f32(staging, 256, row, side * 8 + i * 4, v[i]);
-                    }
-                }
-                if (pass == passes - 1) release();
-                epilogue_sync();
-                const int s0 = chunk * width + pass * 64 + (tid & 7) * 8;
+                const int s0 = first + pass * 64 + (tid & 7) * 8;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int r = (i * 256 + tid) >> 3;
@@ -612,17 +638,16 @@ rows_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUte
                     const __nv_bfloat16* from = p.hidden + place * 2 * p.s + s0;
                     const uint4 hg = pass == 0 ? kept[i][0] : *reinterpret_cast<const uint4*>(from);
                     const uint4 hu = pass == 0 ? kept[i][1] : *reinterpret_cast<const uint4*>(from + p.s);
-                    const int pair = ctl->pair[r];
-                    const float gate = pair >= 0 ? p.gate[pair] : 0.f;
+                    const float g_r = ctl->gate[r];
                     const uint32_t wg[4] = {hg.x, hg.y, hg.z, hg.w}, wu[4] = {hu.x, hu.y, hu.z, hu.w};
                     float c[8], out_g[8], out_u[8], out_a[8];
-                    unstage8(staging_at, 256, r, (tid & 7) * 2, c);
+                    unstage8(staging_at + pass * kTileRows * 256, 256, r, (tid & 7) * 2, c);
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
                         const float g = j & 1 ? bf16_hi(wg[j / 2]) : bf16_lo(wg[j / 2]), up = j & 1 ? bf16_hi(wu[j / 2]) : bf16_lo(wu[j / 2]);
-                        const float sg = sigmoidf(g), silu = g * sg, act = silu * up, da = gate * c[j];
+                        const float sg = sigmoidf(g), silu = g * sg, act = silu * up, da = g_r * c[j];
                         dg[i] = fmaf(c[j], act, dg[i]);
-                        out_a[j] = gate * act;
+                        out_a[j] = g_r * act;
                         out_u[j] = da * silu;
                         out_g[j] = da * up * fmaf(silu, 1.f - sg, sg);
                     }
@@ -630,15 +655,14 @@ rows_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUte
                     *reinterpret_cast<uint4*>(p.du + place * 2 * p.s + p.s + s0) = pack8(out_u);
                     if (p.ga) *reinterpret_cast<uint4*>(p.ga + place * p.s + s0) = pack8(out_a);
                 }
-                if (pass < passes - 1) epilogue_sync();
             }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {                       // the eight threads of a row
+            for (int i = 0; i < 4; ++i) {                           // the eight threads of a row
                 const int r = (i * 256 + tid) >> 3;
 #pragma unroll
                 for (int o = 4; o > 0; o >>= 1) dg[i] += __shfl_xor_sync(0xffffffffu, dg[i], o);
                 const int pair = r < rows ? ctl->pair[r] : -1;
-                if ((tid & 7) == 0 && pair >= 0) p.dgate_part[(long long)chunk * p.P + pair] = dg[i];
+                if ((tid & 7) == 0 && pair >= 0) p.dgate_part[(long long)u.chunk * p.P + pair] = dg[i];
             }
             epilogue_sync();
         }
@@ -1025,7 +1049,7 @@ long long tile_capacity(int T, int M, int k)
 struct Workspace {                 // offsets of the pieces, and the total
     size_t act = 0, du = 0, ga = 0, dgate = 0, dx = 0, dx_scale = 0, total = 0;
 };
-int back_boxes(int s) { return s > 192 ? 4 : (s + 63) / 64; }      // boxes of s rows per unit of the activation's backward
+int back_boxes(int s) { return s > 64 ? 2 : 1; }                    // boxes of s rows per unit of the activation's backward: their sums fit staging
 int row_boxes(int h) { return h > 128 ? 4 : (h > 64 ? 2 : 1); }
 
 Workspace lay_out(int T, int h, int s, int M, int k, bool backward)
