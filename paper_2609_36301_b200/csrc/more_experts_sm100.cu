@@ -32,16 +32,21 @@ namespace more {
 namespace {
 
 // Warp 1 issues the MMAs, warps 2..9 are the epilogue, warp 0 and those from 10 on load: stage n is the (n mod loaders)th one's, as
-// opening a stage and issuing its loads costs a warp 700 to 3000 clocks, several times what a stage may take.
+// opening a stage and issuing its loads costs a warp 700 to 3000 clocks, several times what a stage may take.  In the forward gather
+// two warps share a stage, and it is there sooner: 58 us instead of 62 for 3001 x 6 pairs of 504 experts, h = 1000, s = 40, 265
+// instead of 279 for 32768 x 8 of 256, h = 512, s = 256, nothing lost elsewhere.  (The backward one was 20 to 50 us slower for
+// 65536 x 4 of 8192, whose stages are small: every loader goes through all stages' places.)
 constexpr int kLoaders = 5, kFewLoaders = 3;         // where rows are gathered; elsewhere
+__host__ __device__ constexpr int team_of(int mode) { return mode == 0 /* kUp */ ? 2 : 1; }   // warps that share a stage
 constexpr int threads_of(int loaders) { return (9 + loaders) * 32; }
+constexpr int rows_threads(int mode) { return threads_of((mode == 0 || mode == 2 ? kLoaders : kFewLoaders) * team_of(mode)); }
 __device__ __forceinline__ int loader_of(int warp) { return warp == 0 ? 0 : warp - 9; }
 constexpr int kTileRows = 128;
 constexpr int kBox = 64 * 128;                       // 64 rows of 64 bf16
 constexpr int kRowPitch = 528;                       // a staged output row: 256 16-bit values, and 16 bytes so that rows fall on other banks
 constexpr int kXStaging = kTileRows * kRowPitch;     // what the epilogue passes from the tensor memory's layout to memory's
-constexpr int kXRing = 154 * 1024;
-constexpr int kXControl = 1536 + kLoaders * 512;
+constexpr int kXRing = 153 * 1024;
+constexpr int kXControl = 1536 + 2 * kLoaders * 512;
 constexpr int kXSmem = kXRing + kXStaging + 1024 /*alignment*/ + kXControl;
 static_assert(kXSmem <= 227 * 1024, "shared memory");
 static_assert(kXStaging >= kTileRows * 128, "an operand of fewer rows than the MMA's 128 is read past its end");
@@ -146,7 +151,7 @@ struct Control {
     int abort;
     int pair[kTileRows];
     float gate[kTileRows];
-    int4 rows[kLoaders][kTileRows / 4];   // of each loader's tile
+    int4 rows[2 * kLoaders][kTileRows / 4];   // of each loader's tile
 };
 static_assert(sizeof(Control) <= kXControl, "control block");
 
@@ -302,12 +307,12 @@ __device__ __forceinline__ uint4 pack8_half(const float (&v)[16], int at, float 
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// Common start of both kernels: barriers, tensor memory.  readers: warps that read an accumulator.  Returns the tensor-memory base.
-__device__ __forceinline__ uint32_t open_cta(Control* c, int readers, int warp)
+// Common start of both kernels: barriers, tensor memory.  loads: warps that share a stage; readers: those that read an accumulator.  Returns the tensor-memory base.
+__device__ __forceinline__ uint32_t open_cta(Control* c, int loads, int readers, int warp)
 {
     if (threadIdx.x == 0) {
         for (int i = 0; i < kSlots; ++i) {
-            mbar_init(smem_u32(&c->full[i]), 1);
+            mbar_init(smem_u32(&c->full[i]), loads);
             mbar_init(smem_u32(&c->empty[i]), 1);
         }
         for (int i = 0; i < 2; ++i) {
@@ -444,7 +449,7 @@ __device__ __forceinline__ uint32_t row_bytes(int rows) { return GATHER ? (uint3
 __device__ __forceinline__ int unlike_boxes(int rows) { return rows <= 32 ? 1 : rows <= 64 ? 2 : 4; }
 
 template <int MODE>
-__global__ void __launch_bounds__(threads_of(MODE == kUp || MODE == kBackAct ? kLoaders : kFewLoaders), 1)
+__global__ void __launch_bounds__(rows_threads(MODE), 1)
 rows_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUtensorMap mw, const __grid_constant__ RowsParams p)
 {
     constexpr bool kGather = MODE == kUp || MODE == kBackAct;       // rows of A are tokens', else places in expert order
@@ -456,21 +461,28 @@ rows_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUte
     Control* ctl = reinterpret_cast<Control*>(staging_at + kXStaging);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     let_next_begin();
-    const uint32_t tmem = open_cta(ctl, kCompute ? 8 : 4, warp);
+    const uint32_t tmem = open_cta(ctl, team_of(MODE), kCompute ? 8 : 4, warp);
     wait_for_previous();
     volatile int* abort_flag = &ctl->abort;
     const int units = p.tiles[0].x * p.chunks;
 
     if (warp == 0 || warp >= 10) {
-        constexpr int kMine = kGather ? kLoaders : kFewLoaders;
-        const int loader = loader_of(warp);
-        int4* rows = ctl->rows[loader];
+        constexpr int kMine = kGather ? kLoaders : kFewLoaders, kMembers = team_of(MODE);
+        const int loader = loader_of(warp) / kMembers, member = loader_of(warp) % kMembers;
+        int4* rows = ctl->rows[loader_of(warp)];
         const uint64_t again = comes_again(), once = p.weights_once ? passes_once() : comes_normally();
         Ring rg;
         bool live = true;
         for (TilesAhead<kGather ? 4 : 0> u(p, units, lane); u.more() && live; u.next()) {
             const uint32_t a_bytes = row_bytes<kGather>(u.tile.z), bytes = a_bytes + p.nb * kBox;
             const int gathers = (u.tile.z + 3) / 4, unlike = unlike_boxes(u.tile.z);
+            uint32_t share = 0;                                     // bytes of this warp's loads
+            if constexpr (kGather) {
+                for (int g = member * 4; g < gathers; g += 4 * kMembers) share += min(4, gathers - g) * 512;
+                share += kMn ? p.nb / kMembers * kBox : member == 0 ? p.nb * kBox : 0;
+            } else {
+                share = bytes;
+            }
             if constexpr (kGather) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i)                         // (a row that does not exist is out of bounds: zeros)
@@ -482,18 +494,18 @@ rows_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUte
                 if (!rg.open(bytes, loader, kMine, ctl, lane, abort_flag, p.status, &at, &live)) continue;
                 const uint32_t full = smem_u32(&ctl->full[rg.slot()]);
                 at += ring;
-                expect_elect(full, (kGather ? gathers * 512 : a_bytes) + p.nb * kBox);
+                expect_elect(full, share);
                 if constexpr (kMn) {
-                    for (int b = 0; b < p.nb; ++b) {
+                    for (int b = member; b < p.nb; b += kMembers) {
                         const int half = p.nb / 2;
                         const int x = MODE == kDown ? (u.chunk * p.nb + b) * 64 : (b < half ? 0 : p.s) + (u.chunk * half + (b < half ? b : b - half)) * 64;
                         tma_load_3d_elect(at + a_bytes + b * kBox, &mw, full, x, ks * 64, u.tile.x, once);
                     }
-                } else {
+                } else if (member == 0) {
                     tma_load_3d_elect(at + a_bytes, &mw, full, ks * 64, u.chunk * p.nb * 64, u.tile.x, once);
                 }
                 if constexpr (kGather) {
-                    for (int g = 0; g < gathers; g += 4)
+                    for (int g = member * 4; g < gathers; g += 4 * kMembers)
                         tma_gather16(at + g * 512, &ma, full, ks * 64, gathers - g, rows[g], rows[g + 1], rows[g + 2], rows[g + 3], again);
                 } else {
                     for (int b = 0; b < 4; ++b) tma_load_2d_elect(at + b * 4096, &ma, full, ks * 64, u.tile.y + (b & (unlike - 1)) * 32);
@@ -753,11 +765,7 @@ rows_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUte
 }
 
 // ------------------------------------------------------------------------------------------------ gradients of the weights
-struct WeightsParams {
-    const int32_t* offsets;
-    const int32_t* pairs;
-    int P, T, M;
-    Divide by_k;
+struct WeightsSide {
     int a_by_token;               // dW1: A = X by token, B = du by place; dW2: A = gate a by place, B = d by token
     int rows, cols;               // of an expert's output: A's columns, B's columns
     int mtiles, chunks, nb, box_rows;
@@ -765,20 +773,30 @@ struct WeightsParams {
     // of the accumulator's lanes then hold the same, and all the warps that read it share the columns.
     __device__ int boxes_of_rows(int mt) const { return rows <= 64 || rows - mt * 128 > 64 ? 2 : 1; }
     __device__ bool twice() const { return rows <= 64; }
+    // staging holds two units' boxes of this output, each in its half
+    __device__ bool by_halves() const { return nb * box_rows * 128 <= kXStaging / 2; }
     __nv_bfloat16* out;           // [M][rows][cols]
+};
+static_assert(kXStaging / 2 % 1024 == 0, "boxes begin on 1024 bytes");
+struct WeightsMaps { CUtensorMap token, place, place16, out; };     // place16: 16 rows high; token, place: one, for gathers
+struct WeightsParams {
+    const int32_t* offsets;
+    const int32_t* pairs;
+    int P, T;
+    Divide by_k;
+    unsigned units0, units;       // units of the first output; of both
+    WeightsSide side[2];
     int* status;
 };
 
 // The runs of a CTA's units in turn, for a converged warp, whose lanes hold those of 32 units; the next 32 are requested when they begin.
 struct Units {
     const WeightsParams& p;
-    uint32_t per_expert, units;
     int lane, index;
-    int e, mt, chunk, lo, n;                                 // of the present unit: expert, tile of rows, chunk of columns, its run
+    int which, e, mt, chunk, lo, n;                          // of the present unit: output, expert, tile of rows, chunk of columns, its run
     int batch_e, batch_rem, raw_lo, raw_hi;                  // this lane's
     int next_e, next_rem, next_lo, next_hi;
-    __device__ explicit Units(const WeightsParams& q) : p(q), per_expert(q.mtiles * q.chunks), units((uint32_t)q.M * per_expert),
-                                                        lane(threadIdx.x & 31), index(-1)
+    __device__ explicit Units(const WeightsParams& q) : p(q), lane(threadIdx.x & 31), index(-1)
     {
         request(0);
         next();
@@ -787,13 +805,15 @@ struct Units {
     {
         const unsigned long long u = blockIdx.x + (unsigned long long)(first + lane) * gridDim.x;
         next_e = next_rem = next_lo = next_hi = 0;
-        if (u >= units) return;
-        next_e = (int)((uint32_t)u / per_expert);
-        next_rem = (int)((uint32_t)u % per_expert);
+        if (u >= p.units) return;
+        const int w = u >= p.units0;
+        const unsigned v = (unsigned)u - (w ? p.units0 : 0u), per_expert = (unsigned)(p.side[w].mtiles * p.side[w].chunks);
+        next_e = (int)(v / per_expert);
+        next_rem = (int)(v % per_expert);
         next_lo = p.offsets[next_e];
         next_hi = p.offsets[next_e + 1];
     }
-    __device__ bool more() const { return blockIdx.x + (unsigned long long)index * gridDim.x < units; }
+    __device__ bool more() const { return blockIdx.x + (unsigned long long)index * gridDim.x < p.units; }
     __device__ void next()
     {
         const int i = ++index & 31;
@@ -804,18 +824,18 @@ struct Units {
             raw_hi = max(min(hold(next_hi), p.P), raw_lo);
             request(index + 32);
         }
+        which = blockIdx.x + (unsigned long long)index * gridDim.x >= p.units0;
         e = __shfl_sync(0xffffffffu, batch_e, i);
-        const int rem = __shfl_sync(0xffffffffu, batch_rem, i);
-        mt = p.chunks == 1 ? rem : rem / p.chunks;
-        chunk = p.chunks == 1 ? 0 : rem % p.chunks;
+        const int rem = __shfl_sync(0xffffffffu, batch_rem, i), chunks = p.side[which].chunks;
+        mt = chunks == 1 ? rem : rem / chunks;
+        chunk = chunks == 1 ? 0 : rem % chunks;
         lo = __shfl_sync(0xffffffffu, raw_lo, i);
         n = __shfl_sync(0xffffffffu, raw_hi, i) - lo;
     }
 };
 
 __global__ void __launch_bounds__(threads_of(kLoaders), 1)
-weights_kernel(const __grid_constant__ CUtensorMap mtoken, const __grid_constant__ CUtensorMap mplace, const __grid_constant__ CUtensorMap mplace16,
-               const __grid_constant__ CUtensorMap mout, const __grid_constant__ WeightsParams p)
+weights_kernel(const __grid_constant__ WeightsMaps m0, const __grid_constant__ WeightsMaps m1, const __grid_constant__ WeightsParams all)
 {
     extern __shared__ uint8_t smem_raw[];
     const uint32_t ring = (smem_u32(smem_raw) + 1023u) & ~1023u, staging = ring + kXRing;
@@ -823,7 +843,7 @@ weights_kernel(const __grid_constant__ CUtensorMap mtoken, const __grid_constant
     Control* ctl = reinterpret_cast<Control*>(staging_at + kXStaging);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     let_next_begin();
-    const uint32_t tmem = open_cta(ctl, 8, warp);
+    const uint32_t tmem = open_cta(ctl, 1, 8, warp);
     wait_for_previous();
     volatile int* abort_flag = &ctl->abort;
 
@@ -838,57 +858,60 @@ weights_kernel(const __grid_constant__ CUtensorMap mtoken, const __grid_constant
         Ring rg;
         bool live = true;
         struct Own {
-            int first, left, mt, chunk, last, slot, pair[2];        // first place, rows; the stage that has to be empty, or less than 0
+            int which, first, left, mt, chunk, last, slot, pair[2];  // output, first place, rows; the stage that has to be empty, or less than 0
             uint32_t where;
         } own;
         own.left = 0;
         auto issue = [&]() {
             if (own.left == 0 || !live) return;
-            const int left = own.left, steps = (left + 15) / 16, a_boxes = p.boxes_of_rows(own.mt);
+            const WeightsSide& o = all.side[own.which];
+            const WeightsMaps& m = own.which ? m1 : m0;
+            const int left = own.left, steps = (left + 15) / 16, a_boxes = o.boxes_of_rows(own.mt);
             const uint32_t box = (uint32_t)steps * 2048;
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 const int r = i * 32 + lane, pair = hold(own.pair[i]);
-                const bool in = pair >= 0 && pair < p.P;
-                reinterpret_cast<int*>(rows)[r] = in ? p.by_k(pair) : p.T;
-                reinterpret_cast<int*>(rows)[64 + r] = in ? own.first + r : p.P;
+                const bool in = pair >= 0 && pair < all.P;
+                reinterpret_cast<int*>(rows)[r] = in ? all.by_k(pair) : all.T;
+                reinterpret_cast<int*>(rows)[64 + r] = in ? own.first + r : all.P;
             }
-            if (own.last >= 0 && !mbar_wait(smem_u32(&ctl->empty[own.last % kSlots]), (own.last / kSlots) & 1, abort_flag, p.status)) {
+            if (own.last >= 0 && !mbar_wait(smem_u32(&ctl->empty[own.last % kSlots]), (own.last / kSlots) & 1, abort_flag, all.status)) {
                 live = false;
                 return;
             }
             __syncwarp();
             const uint32_t full = smem_u32(&ctl->full[own.slot]);
-            expect_elect(full, box * (a_boxes + p.nb));
+            expect_elect(full, box * (a_boxes + o.nb));
             const uint32_t a_at = ring + own.where, b_at = a_at + a_boxes * box;
-            const int a_x = own.mt * 128, b_x = own.chunk * p.nb * 64;
-            const int t_boxes = p.a_by_token ? a_boxes : p.nb, p_boxes = p.a_by_token ? p.nb : a_boxes;
-            const int t_x = p.a_by_token ? a_x : b_x, p_x = p.a_by_token ? b_x : a_x;
-            const int t_step = p.a_by_token && p.twice() ? 0 : 64, p_step = !p.a_by_token && p.twice() ? 0 : 64;
-            const uint32_t t_at = p.a_by_token ? a_at : b_at, p_at = p.a_by_token ? b_at : a_at;
+            const int a_x = own.mt * 128, b_x = own.chunk * o.nb * 64;
+            const int t_boxes = o.a_by_token ? a_boxes : o.nb, p_boxes = o.a_by_token ? o.nb : a_boxes;
+            const int t_x = o.a_by_token ? a_x : b_x, p_x = o.a_by_token ? b_x : a_x;
+            const int t_step = o.a_by_token && o.twice() ? 0 : 64, p_step = !o.a_by_token && o.twice() ? 0 : 64;
+            const uint32_t t_at = o.a_by_token ? a_at : b_at, p_at = o.a_by_token ? b_at : a_at;
             for (int q = 0; q < steps; ++q) {
                 const int4 r0 = rows[4 * q], r1 = rows[4 * q + 1], r2 = rows[4 * q + 2], r3 = rows[4 * q + 3];
-                for (int b = 0; b < t_boxes; ++b) tma_gather16(t_at + b * box + q * 2048, &mtoken, full, t_x + b * t_step, 4, r0, r1, r2, r3, again);
+                for (int b = 0; b < t_boxes; ++b) tma_gather16(t_at + b * box + q * 2048, &m.token, full, t_x + b * t_step, 4, r0, r1, r2, r3, again);
                 if (left >= q * 16 + 16) {
-                    for (int b = 0; b < p_boxes; ++b) tma_load_2d_elect(p_at + b * box + q * 2048, &mplace16, full, p_x + b * p_step, own.first + q * 16);
+                    for (int b = 0; b < p_boxes; ++b) tma_load_2d_elect(p_at + b * box + q * 2048, &m.place16, full, p_x + b * p_step, own.first + q * 16);
                 } else {
                     const int4 s0 = rows[16 + 4 * q], s1 = rows[17 + 4 * q], s2 = rows[18 + 4 * q], s3 = rows[19 + 4 * q];
-                    for (int b = 0; b < p_boxes; ++b) tma_gather16(p_at + b * box + q * 2048, &mplace, full, p_x + b * p_step, 4, s0, s1, s2, s3, again);
+                    for (int b = 0; b < p_boxes; ++b) tma_gather16(p_at + b * box + q * 2048, &m.place, full, p_x + b * p_step, 4, s0, s1, s2, s3, again);
                 }
             }
             __syncwarp();                                           // (the rows are read)
         };
-        for (Units u(p); u.more() && live; u.next()) {
-            const int a_boxes = p.boxes_of_rows(u.mt);
+        for (Units u(all); u.more() && live; u.next()) {
+            const int a_boxes = all.side[u.which].boxes_of_rows(u.mt), nb = all.side[u.which].nb;
             for (int at = 0; at < u.n; at += 64, ++rg.n) {
                 const int left = min(64, u.n - at);
                 uint32_t where;
                 int last;
-                if (!rg.mine((uint32_t)((left + 15) / 16) * 2048 * (a_boxes + p.nb), loader, kLoaders, lane, &where, &last)) continue;
+                if (!rg.mine((uint32_t)((left + 15) / 16) * 2048 * (a_boxes + nb), loader, kLoaders, lane, &where, &last)) continue;
                 int pair[2];
 #pragma unroll
-                for (int i = 0; i < 2; ++i) pair[i] = i * 32 + lane < left ? p.pairs[u.lo + at + i * 32 + lane] : -1;
+                for (int i = 0; i < 2; ++i) pair[i] = i * 32 + lane < left ? all.pairs[u.lo + at + i * 32 + lane] : -1;
                 issue();
+                own.which = u.which;
                 own.first = u.lo + at;
                 own.left = left;
                 own.mt = u.mt;
@@ -902,22 +925,22 @@ weights_kernel(const __grid_constant__ CUtensorMap mtoken, const __grid_constant
         }
         issue();
     } else if (warp == 1) {
-        const uint32_t idesc = idesc_of(p.nb * 64, 1, 1);
         const uint64_t d0 = umma_desc_sw128(ring, 0, 1024);
         Ring rg;
         int it = 0;
         bool live = true;
-        for (Units u(p); u.more() && live; u.next()) {
+        for (Units u(all); u.more() && live; u.next()) {
             const int n = u.n;
             if (n == 0) continue;                                   // (the epilogue writes zeros without an accumulator)
-            const int buf = it & 1, a_boxes = p.boxes_of_rows(u.mt);
-            if (!mbar_wait(smem_u32(&ctl->acc_empty[buf]), ((it >> 1) & 1) ^ 1u, abort_flag, p.status)) break;
+            const int buf = it & 1, a_boxes = all.side[u.which].boxes_of_rows(u.mt), nb = all.side[u.which].nb;
+            const uint32_t idesc = idesc_of(nb * 64, 1, 1);
+            if (!mbar_wait(smem_u32(&ctl->acc_empty[buf]), ((it >> 1) & 1) ^ 1u, abort_flag, all.status)) break;
             tc_fence_after();
             for (int at = 0; at < n; at += 64) {
                 const uint32_t steps = (min(64, n - at) + 15) / 16, box = steps * 2048;
                 uint32_t from;
-                const uint32_t off = rg.place(box * (a_boxes + p.nb), &from);
-                if (!mbar_wait(smem_u32(&ctl->full[rg.slot()]), rg.parity(), abort_flag, p.status)) { live = false; break; }
+                const uint32_t off = rg.place(box * (a_boxes + nb), &from);
+                if (!mbar_wait(smem_u32(&ctl->full[rg.slot()]), rg.parity(), abort_flag, all.status)) { live = false; break; }
                 tc_fence_after();
                 // boxes lie `box` apart: the distance of 64 columns in both descriptors
                 const uint32_t a_lo = ((uint32_t)d0 + (off >> 4)) | (box >> 4) << 16, b_lo = a_lo + (a_boxes * box >> 4), hi = (uint32_t)(d0 >> 32);
@@ -933,11 +956,13 @@ weights_kernel(const __grid_constant__ CUtensorMap mtoken, const __grid_constant
         // bf16 boxes of 64 columns in the layout of a swizzled TMA store, which cuts off what is behind the ends, of 128 rows, or of 64
         // where no more are needed; two units' worth of them where staging holds that
         const int quarter = warp & 3, side = warp >= 6, tid = threadIdx.x - 64;
-        const int copies = p.twice() ? 2 : 1, copy = p.twice() ? quarter >> 1 : 0, row0 = (p.twice() ? quarter & 1 : quarter) * 32, row = row0 + lane;
         const uint64_t once = passes_once();
-        const int box = p.box_rows * 128, buffers = 2 * p.nb * box <= kXStaging ? 2 : 1;
         int it = 0;
-        for (Units w(p); w.more(); w.next()) {
+        bool halves = true;                                         // the unit before kept to its half of staging
+        for (Units w(all); w.more(); w.next()) {
+            const WeightsSide& p = all.side[w.which];
+            const int copies = p.twice() ? 2 : 1, copy = p.twice() ? quarter >> 1 : 0, row0 = (p.twice() ? quarter & 1 : quarter) * 32, row = row0 + lane;
+            const int box = p.box_rows * 128;
             const int mt = w.mt, per = p.nb * 32, c0 = w.chunk * p.nb * 64;
             const int rows = min(128, p.rows - mt * 128);
             if (w.n == 0) {                                         // zeros: threads along rows, 16 bytes each
@@ -949,10 +974,11 @@ weights_kernel(const __grid_constant__ CUtensorMap mtoken, const __grid_constant
                 continue;
             }
             const int buf = it & 1;
-            const uint32_t acc = tmem + buf * 256 + ((uint32_t)(quarter * 32) << 16), to = staging + (it & (buffers - 1)) * p.nb * box;
-            const bool ok = mbar_wait(smem_u32(&ctl->acc_full[buf]), (it >> 1) & 1, abort_flag, p.status);   // (given up: goes on without work)
+            const uint32_t acc = tmem + buf * 256 + ((uint32_t)(quarter * 32) << 16), to = staging + (p.by_halves() ? (it & 1) * (kXStaging / 2) : 0);
+            const bool ok = mbar_wait(smem_u32(&ctl->acc_full[buf]), (it >> 1) & 1, abort_flag, all.status);   // (given up: goes on without work)
             tc_fence_after();
-            if (warp == 2) buffers == 2 ? bulk_read_done<1>() : bulk_read_done<0>();
+            if (warp == 2) halves && p.by_halves() ? bulk_read_done<1>() : bulk_read_done<0>();
+            halves = p.by_halves();
             epilogue_sync();
             for (int c = copy * 32; ok && c < per && row0 < rows && c0 + side * per + c < p.cols; c += copies * 32) {
                 float v[2][16];
@@ -972,7 +998,7 @@ weights_kernel(const __grid_constant__ CUtensorMap mtoken, const __grid_constant
             fence_async_smem();
             epilogue_sync();
             if (warp == 2) {
-                for (int b = 0; ok && b < p.nb && c0 + b * 64 < p.cols; ++b) tma_store_3d_elect(&mout, to + b * box, c0 + b * 64, mt * 128, w.e, once);
+                for (int b = 0; ok && b < p.nb && c0 + b * 64 < p.cols; ++b) tma_store_3d_elect(w.which ? &m1.out : &m0.out, to + b * box, c0 + b * 64, mt * 128, w.e, once);
                 bulk_commit();
             }
         }
@@ -1101,7 +1127,7 @@ int launch_rows(const CUtensorMap& ma, const CUtensorMap& mw, RowsParams p, long
     const long long units = tiles * p.chunks;
     if (units > 0x7fff0000LL) return MORE_ERR_TOO_LARGE;
     const int grid = units < ctx.sm_count ? (int)units : ctx.sm_count;
-    const int threads = threads_of(MODE == kUp || MODE == kBackAct ? kLoaders : kFewLoaders);
+    const int threads = rows_threads(MODE);
     if (launch_behind(rows_kernel<MODE>, grid, threads, kXSmem, st, ma, mw, p) != cudaSuccess) return MORE_ERR_CUDA;
     count_launch(1);
     return MORE_OK;
@@ -1115,22 +1141,43 @@ int launch_tiles(const ExpertsArgs& a, cudaStream_t st)
     return cudaGetLastError() == cudaSuccess ? MORE_OK : MORE_ERR_CUDA;
 }
 
-int launch_weights(const CUtensorMap& mtoken, const CUtensorMap (&mplace)[2], WeightsParams p, const DeviceCtx& ctx, cudaStream_t st)
+// dW1, dW2 or both, in one launch: what one leaves idle at its end, the other uses.
+int launch_weights(const ExpertsArgs& a, const Workspace& w, const DeviceCtx& ctx)
 {
-    CUtensorMap mout;
-    p.box_rows = p.rows > 64 ? 128 : 64;
-    const int rc = weight_map(p.out, p.M, p.rows, p.cols, p.box_rows, &mout);
-    if (rc != MORE_OK) return rc;
-    if (allow_smem(weights_kernel) != MORE_OK) return MORE_ERR_CUDA;
-    p.nb = p.cols > 128 ? 4 : (p.cols > 64 ? 2 : 1);
-    p.mtiles = (p.rows + 127) / 128;
-    p.chunks = (p.cols + p.nb * 64 - 1) / (p.nb * 64);
+    const long long P = (long long)a.T * a.k;
+    char* base = static_cast<char*>(a.workspace);
+    WeightsMaps m[2] = {};
+    WeightsParams p{};
+    p.offsets = a.offsets; p.pairs = a.pairs; p.P = (int)P; p.T = a.T; p.by_k.by(a.k);
     p.status = ctx.status;
-    const long long units = (long long)p.M * p.mtiles * p.chunks;
-    if (units > 0x7fff0000LL) return MORE_ERR_TOO_LARGE;
+    long long units = 0;
+    int n = 0;
+    for (int i = 0; i < 2; ++i) {
+        __nv_bfloat16* const out = i == 0 ? a.out_dw1 : a.out_dw2;
+        if (!out) continue;
+        WeightsSide& o = p.side[n];
+        o.a_by_token = i == 0;
+        o.rows = i == 0 ? a.h : a.s; o.cols = i == 0 ? 2 * a.s : a.h; o.out = out;
+        o.box_rows = o.rows > 64 ? 128 : 64;
+        o.nb = row_boxes(o.cols);
+        o.mtiles = (o.rows + 127) / 128;
+        o.chunks = (o.cols + o.nb * 64 - 1) / (o.nb * 64);
+        const char* place = base + (i == 0 ? w.du : w.ga);
+        const int width = i == 0 ? 2 * a.s : a.s;
+        int rc = rows_map(i == 0 ? a.X : a.dout, a.T, a.h, 1, &m[n].token);
+        if (rc == MORE_OK) rc = rows_map(place, P, width, 1, &m[n].place);
+        if (rc == MORE_OK) rc = rows_map(place, P, width, 16, &m[n].place16);
+        if (rc == MORE_OK) rc = weight_map(out, a.M, o.rows, o.cols, o.box_rows, &m[n].out);
+        if (rc != MORE_OK) return rc;
+        units += (long long)a.M * o.mtiles * o.chunks;
+        if (n++ == 0) p.units0 = (unsigned)units;
+        if (units > 0x7fff0000LL) return MORE_ERR_TOO_LARGE;
+    }
+    if (n == 0) return MORE_OK;
+    p.units = (unsigned)units;
+    if (allow_smem(weights_kernel) != MORE_OK) return MORE_ERR_CUDA;
     const int grid = units < ctx.sm_count ? (int)units : ctx.sm_count;
-    if (launch_behind(weights_kernel, grid, threads_of(kLoaders), kXSmem, st, mtoken, mplace[0], mplace[1], mout, p) != cudaSuccess)
-        return MORE_ERR_CUDA;
+    if (launch_behind(weights_kernel, grid, threads_of(kLoaders), kXSmem, a.stream, m[0], m[1], p) != cudaSuccess) return MORE_ERR_CUDA;
     count_launch(1);
     return MORE_OK;
 }
@@ -1174,12 +1221,9 @@ int launch_experts_backward(const ExpertsArgs& a, const DeviceCtx& ctx)
     const long long P = (long long)a.T * a.k;
     const Workspace w = lay_out(a.T, a.h, a.s, a.M, a.k, true);
     char* base = static_cast<char*>(a.workspace);
-    CUtensorMap mx, md, mdu[2], mdu32, mga[2], m1, m2;             // rows by token; by place one row, 16 and 32 rows high; weights
-    int rc = rows_map(a.X, a.T, a.h, 1, &mx);
-    if (rc == MORE_OK) rc = rows_map(a.dout, a.T, a.h, 1, &md);
-    for (int i = 0; i < 2 && rc == MORE_OK; ++i) rc = rows_map(base + w.du, P, 2 * a.s, i == 0 ? 1 : 16, &mdu[i]);
-    if (rc == MORE_OK) rc = rows_map(base + w.du, P, 2 * a.s, 32, &mdu32);
-    for (int i = 0; i < 2 && rc == MORE_OK; ++i) rc = rows_map(base + w.ga, P, a.s, i == 0 ? 1 : 16, &mga[i]);
+    CUtensorMap md, mdu, m1, m2;
+    int rc = rows_map(a.dout, a.T, a.h, 1, &md);
+    if (rc == MORE_OK) rc = rows_map(base + w.du, P, 2 * a.s, 32, &mdu);
     if (rc == MORE_OK) rc = weight_map(a.W1, a.M, a.h, 2 * a.s, row_boxes(a.h) * 64, &m1);
     if (rc == MORE_OK) rc = weight_map(a.W2, a.M, a.s, a.h, back_boxes(a.s) * 64, &m2);
     if (rc == MORE_OK) rc = launch_tiles(a, a.stream);
@@ -1211,7 +1255,7 @@ int launch_experts_backward(const ExpertsArgs& a, const DeviceCtx& ctx)
         p.nb = row_boxes(a.h);
         p.chunks = (a.h + p.nb * 64 - 1) / (p.nb * 64);
         p.ksteps = (2 * a.s + 63) / 64;
-        rc = launch_rows<kBackX>(mdu32, m1, p, tiles, ctx, a.stream);
+        rc = launch_rows<kBackX>(mdu, m1, p, tiles, ctx, a.stream);
         if (rc != MORE_OK) return rc;
     }
     if (a.out_dx || a.out_dgate) {
@@ -1224,20 +1268,7 @@ int launch_experts_backward(const ExpertsArgs& a, const DeviceCtx& ctx)
         if (launch_behind(join_kernel, (int)(blocks < 148 * 16 ? blocks : 148 * 16), 256, 0, a.stream, j) != cudaSuccess) return MORE_ERR_CUDA;
         count_launch(1);
     }
-    WeightsParams q{};
-    q.offsets = a.offsets; q.pairs = a.pairs; q.P = (int)P; q.T = a.T; q.by_k.by(a.k); q.M = a.M;
-    if (a.out_dw1) {
-        q.a_by_token = 1;
-        q.rows = a.h; q.cols = 2 * a.s; q.out = a.out_dw1;
-        rc = launch_weights(mx, mdu, q, ctx, a.stream);
-        if (rc != MORE_OK) return rc;
-    }
-    if (a.out_dw2) {
-        q.a_by_token = 0;
-        q.rows = a.s; q.cols = a.h; q.out = a.out_dw2;
-        rc = launch_weights(md, mga, q, ctx, a.stream);
-    }
-    return rc;
+    return launch_weights(a, w, ctx);
 }
 
 int check_sizes(int T, int h, int s, int M, int k)
