@@ -787,6 +787,20 @@ struct WeightsParams {
     unsigned units0, units;       // units of the first output; of both
     WeightsSide side[2];
     int* status;
+    // (by selects: an index would make each field a load of its own)
+    __device__ WeightsSide of(int which) const
+    {
+        WeightsSide o;
+        o.a_by_token = which ? side[1].a_by_token : side[0].a_by_token;
+        o.rows = which ? side[1].rows : side[0].rows;
+        o.cols = which ? side[1].cols : side[0].cols;
+        o.mtiles = which ? side[1].mtiles : side[0].mtiles;
+        o.chunks = which ? side[1].chunks : side[0].chunks;
+        o.nb = which ? side[1].nb : side[0].nb;
+        o.box_rows = which ? side[1].box_rows : side[0].box_rows;
+        o.out = which ? side[1].out : side[0].out;
+        return o;
+    }
 };
 
 // The runs of a CTA's units in turn, for a converged warp, whose lanes hold those of 32 units; the next 32 are requested when they begin.
@@ -807,7 +821,7 @@ struct Units {
         next_e = next_rem = next_lo = next_hi = 0;
         if (u >= p.units) return;
         const int w = u >= p.units0;
-        const unsigned v = (unsigned)u - (w ? p.units0 : 0u), per_expert = (unsigned)(p.side[w].mtiles * p.side[w].chunks);
+        const unsigned v = (unsigned)u - (w ? p.units0 : 0u), per_expert = (unsigned)(p.of(w).mtiles * p.of(w).chunks);
         next_e = (int)(v / per_expert);
         next_rem = (int)(v % per_expert);
         next_lo = p.offsets[next_e];
@@ -826,7 +840,7 @@ struct Units {
         }
         which = blockIdx.x + (unsigned long long)index * gridDim.x >= p.units0;
         e = __shfl_sync(0xffffffffu, batch_e, i);
-        const int rem = __shfl_sync(0xffffffffu, batch_rem, i), chunks = p.side[which].chunks;
+        const int rem = __shfl_sync(0xffffffffu, batch_rem, i), chunks = p.of(which).chunks;
         mt = chunks == 1 ? rem : rem / chunks;
         chunk = chunks == 1 ? 0 : rem % chunks;
         lo = __shfl_sync(0xffffffffu, raw_lo, i);
@@ -864,7 +878,7 @@ weights_kernel(const __grid_constant__ WeightsMaps m0, const __grid_constant__ W
         own.left = 0;
         auto issue = [&]() {
             if (own.left == 0 || !live) return;
-            const WeightsSide& o = all.side[own.which];
+            const WeightsSide o = all.of(own.which);
             const WeightsMaps& m = own.which ? m1 : m0;
             const int left = own.left, steps = (left + 15) / 16, a_boxes = o.boxes_of_rows(own.mt);
             const uint32_t box = (uint32_t)steps * 2048;
@@ -901,7 +915,7 @@ weights_kernel(const __grid_constant__ WeightsMaps m0, const __grid_constant__ W
             __syncwarp();                                           // (the rows are read)
         };
         for (Units u(all); u.more() && live; u.next()) {
-            const int a_boxes = all.side[u.which].boxes_of_rows(u.mt), nb = all.side[u.which].nb;
+            const int a_boxes = all.of(u.which).boxes_of_rows(u.mt), nb = all.of(u.which).nb;
             for (int at = 0; at < u.n; at += 64, ++rg.n) {
                 const int left = min(64, u.n - at);
                 uint32_t where;
@@ -932,7 +946,7 @@ weights_kernel(const __grid_constant__ WeightsMaps m0, const __grid_constant__ W
         for (Units u(all); u.more() && live; u.next()) {
             const int n = u.n;
             if (n == 0) continue;                                   // (the epilogue writes zeros without an accumulator)
-            const int buf = it & 1, a_boxes = all.side[u.which].boxes_of_rows(u.mt), nb = all.side[u.which].nb;
+            const int buf = it & 1, a_boxes = all.of(u.which).boxes_of_rows(u.mt), nb = all.of(u.which).nb;
             const uint32_t idesc = idesc_of(nb * 64, 1, 1);
             if (!mbar_wait(smem_u32(&ctl->acc_empty[buf]), ((it >> 1) & 1) ^ 1u, abort_flag, all.status)) break;
             tc_fence_after();
@@ -960,7 +974,7 @@ weights_kernel(const __grid_constant__ WeightsMaps m0, const __grid_constant__ W
         int it = 0;
         bool halves = true;                                         // the unit before kept to its half of staging
         for (Units w(all); w.more(); w.next()) {
-            const WeightsSide& p = all.side[w.which];
+            const WeightsSide p = all.of(w.which);
             const int copies = p.twice() ? 2 : 1, copy = p.twice() ? quarter >> 1 : 0, row0 = (p.twice() ? quarter & 1 : quarter) * 32, row = row0 + lane;
             const int box = p.box_rows * 128;
             const int mt = w.mt, per = p.nb * 32, c0 = w.chunk * p.nb * 64;
