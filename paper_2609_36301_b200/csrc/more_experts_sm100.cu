@@ -448,6 +448,13 @@ __device__ __forceinline__ uint32_t row_bytes(int rows) { return GATHER ? (uint3
 // read by warps of its own, which then share the columns.  How many of the four boxes differ:
 __device__ __forceinline__ int unlike_boxes(int rows) { return rows <= 32 ? 1 : rows <= 64 ? 2 : 4; }
 
+// Steps of 64 columns per stage, of `bytes` each.  The warp that issues the MMAs spends about 400 clocks on a stage, more than the 64
+// columns of a small tile of kBackAct take to come: two of those make a stage (156 us instead of 170 for the activation's backward of
+// 65536 x 4 pairs of 8192 experts, h = 512, s = 64; up to 24 KB gained no more there and cost 2 % on tiles of 128 rows; in kUp,
+// whose weights weigh twice as much, it cost 2 %).
+template <int MODE>
+__device__ __forceinline__ int stage_steps(uint32_t bytes, int left) { return MODE == kBackAct && bytes <= 16 * 1024 && left > 1 ? 2 : 1; }
+
 template <int MODE>
 __global__ void __launch_bounds__(rows_threads(MODE), 1)
 rows_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUtensorMap mw, const __grid_constant__ RowsParams p)
@@ -489,26 +496,30 @@ rows_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUte
                     reinterpret_cast<int*>(rows)[i * 32 + lane] = u.pair[i] < 0 ? p.rows : p.by_k(u.pair[i]);
                 __syncwarp();
             }
-            for (int ks = 0; ks < p.ksteps && live; ++ks, ++rg.n) {
+            for (int ks = 0, steps; ks < p.ksteps && live; ks += steps, ++rg.n) {
                 uint32_t at;
-                if (!rg.open(bytes, loader, kMine, ctl, lane, abort_flag, p.status, &at, &live)) continue;
+                steps = stage_steps<MODE>(bytes, p.ksteps - ks);
+                if (!rg.open(steps * bytes, loader, kMine, ctl, lane, abort_flag, p.status, &at, &live)) continue;
                 const uint32_t full = smem_u32(&ctl->full[rg.slot()]);
                 at += ring;
-                expect_elect(full, share);
-                if constexpr (kMn) {
-                    for (int b = member; b < p.nb; b += kMembers) {
-                        const int half = p.nb / 2;
-                        const int x = MODE == kDown ? (u.chunk * p.nb + b) * 64 : (b < half ? 0 : p.s) + (u.chunk * half + (b < half ? b : b - half)) * 64;
-                        tma_load_3d_elect(at + a_bytes + b * kBox, &mw, full, x, ks * 64, u.tile.x, once);
+                expect_elect(full, steps * share);
+                for (int i = 0; i < steps; ++i, at += bytes) {
+                    const int x_k = (ks + i) * 64;
+                    if constexpr (kMn) {
+                        for (int b = member; b < p.nb; b += kMembers) {
+                            const int half = p.nb / 2;
+                            const int x = MODE == kDown ? (u.chunk * p.nb + b) * 64 : (b < half ? 0 : p.s) + (u.chunk * half + (b < half ? b : b - half)) * 64;
+                            tma_load_3d_elect(at + a_bytes + b * kBox, &mw, full, x, x_k, u.tile.x, once);
+                        }
+                    } else if (member == 0) {
+                        tma_load_3d_elect(at + a_bytes, &mw, full, x_k, u.chunk * p.nb * 64, u.tile.x, once);
                     }
-                } else if (member == 0) {
-                    tma_load_3d_elect(at + a_bytes, &mw, full, ks * 64, u.chunk * p.nb * 64, u.tile.x, once);
-                }
-                if constexpr (kGather) {
-                    for (int g = member * 4; g < gathers; g += 4 * kMembers)
-                        tma_gather16(at + g * 512, &ma, full, ks * 64, gathers - g, rows[g], rows[g + 1], rows[g + 2], rows[g + 3], again);
-                } else {
-                    for (int b = 0; b < 4; ++b) tma_load_2d_elect(at + b * 4096, &ma, full, ks * 64, u.tile.y + (b & (unlike - 1)) * 32);
+                    if constexpr (kGather) {
+                        for (int g = member * 4; g < gathers; g += 4 * kMembers)
+                            tma_gather16(at + g * 512, &ma, full, x_k, gathers - g, rows[g], rows[g + 1], rows[g + 2], rows[g + 3], again);
+                    } else {
+                        for (int b = 0; b < 4; ++b) tma_load_2d_elect(at + b * 4096, &ma, full, x_k, u.tile.y + (b & (unlike - 1)) * 32);
+                    }
                 }
             }
             __syncwarp();                                           // (the rows are read)
@@ -523,7 +534,8 @@ rows_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUte
         bool live = true;
         for (TilesAhead<0> u(p, units, 0); u.more() && live; u.next()) {
             const uint32_t a_bytes = row_bytes<kGather>(u.tile.z), bytes = a_bytes + p.nb * kBox;
-            for (int ks = 0; ks < p.ksteps; ++ks) {
+            for (int ks = 0, steps; ks < p.ksteps; ks += steps) {
+                steps = stage_steps<MODE>(bytes, p.ksteps - ks);
                 const int in_block = MODE == kBackAct ? ks % kSumSteps : ks;
                 const uint32_t d = tmem + (it & 1) * 256;
                 if (in_block == 0) {
@@ -531,16 +543,18 @@ rows_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUte
                     tc_fence_after();
                 }
                 uint32_t from;
-                const uint32_t off = rg.place(bytes, &from);
+                const uint32_t off = rg.place(steps * bytes, &from);
                 if (!mbar_wait(smem_u32(&ctl->full[rg.slot()]), rg.parity(), abort_flag, p.status)) { live = false; break; }
                 tc_fence_after();
-                const uint32_t al = (uint32_t)a0 + (off >> 4), bl = (uint32_t)b0 + ((off + a_bytes) >> 4);
+                uint32_t al = (uint32_t)a0 + (off >> 4), bl = (uint32_t)b0 + ((off + a_bytes) >> 4);
+                for (int i = 0; i < steps; ++i, al += bytes >> 4, bl += bytes >> 4) {
 #pragma unroll
-                for (int q = 0; q < 4; ++q)
-                    tc_mma_bf16_ss_elect(d, al + q * 2, a_hi, bl + q * kBStep, b_hi, idesc, in_block > 0 || q > 0);
+                    for (int q = 0; q < 4; ++q)
+                        tc_mma_bf16_ss_elect(d, al + q * 2, a_hi, bl + q * kBStep, b_hi, idesc, in_block > 0 || i > 0 || q > 0);
+                }
                 tc_commit_elect(smem_u32(&ctl->empty[rg.slot()]));
                 ++rg.n;
-                if (ks == p.ksteps - 1 || (MODE == kBackAct && in_block == kSumSteps - 1)) {
+                if (ks + steps == p.ksteps || (MODE == kBackAct && in_block + steps == kSumSteps)) {
                     tc_commit_elect(smem_u32(&ctl->acc_full[it & 1]));
                     ++it;
                 }
