@@ -162,7 +162,7 @@ __global__ void __launch_bounds__(WIDE ? 512 : 256) combine_kernel(const __grid_
         __syncthreads();
     }
     const int lane = WIDE ? threadIdx.x : threadIdx.x & 31, width = WIDE ? blockDim.x : 32;
-    const int t = WIDE ? blockIdx.x : blockIdx.x * 8 + (threadIdx.x >> 5);
+    const int t = (int)(WIDE ? blockIdx.x : blockIdx.x * 8 + (threadIdx.x >> 5));      // (T <= 2^31 - 1: at most 2^31 - 1)
     if (!WIDE && t >= p.T) return;
     float y[NV][8], r[NV][8];
     bool live[NV];
@@ -295,7 +295,7 @@ __global__ void __launch_bounds__(512) combine_ring_kernel(const __grid_constant
     const int lane = tid & 31;
     auto gate_of = [&](long long t) { return lane < p.k && t < p.T ? (p.gate ? p.gate[t * p.k + lane] : 1.f) : 0.f; };
     float next_gate = gate_of(blockIdx.x);
-    int stage = 0;
+    int stage = 0, turn = 0;
     uint32_t phase = 0;
     for (long long t = blockIdx.x; t < p.T; t += gridDim.x) {
         const float gates = next_gate;
@@ -333,7 +333,8 @@ __global__ void __launch_bounds__(512) combine_ring_kernel(const __grid_constant
         float inv = 1.f;
         if (p.w_post) {
             float q[1] = {both(a)};
-            token_sum<true>(q, sums[0]);
+            token_sum<true>(q, sums[turn]);
+            if (!p.out_x) turn ^= 1;                         // (no other sum's barrier before the next token's)
             inv = rsqrtf(fmaf(q[0], p.inv_h, p.eps));
         } else {
             __syncthreads();
@@ -388,7 +389,7 @@ struct CombineBackParams {
 
 // A CTA goes through every gridDim.x-th token.  The rows of the next tokens are on their way into a ring in shared memory (bulk copies,
 // a row each) while one is worked on: the two sums over a row that have to be known before anything can be written are chains of
-// latency, which left the memory idle half of the time when rows came by loads into registers (519 us at 65536 x 2048, now 284).
+// latency, which left the memory idle half of the time when rows came by loads into registers (519 us at 65536 x 2048, now 290).
 template <int NV, class R, int THREADS>
 __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) combine_back_kernel(const __grid_constant__ CombineBackParams p)
 {
@@ -632,7 +633,7 @@ int launch_ring(const CombineParams& p, int* status, cudaStream_t st, bool* done
 template <int NV, bool WIDE, class R>
 void launch_forward(const CombineParams& p, int width, cudaStream_t st)
 {
-    combine_kernel<NV, WIDE, R><<<WIDE ? p.T : (p.T + 7) / 8, WIDE ? width : 256, 0, st>>>(p);
+    combine_kernel<NV, WIDE, R><<<WIDE ? (unsigned)p.T : ((unsigned)p.T + 7) / 8, WIDE ? width : 256, 0, st>>>(p);
 }
 
 }  // namespace
@@ -714,7 +715,8 @@ int more_combine_backward(const void* dresidual, const void* dx, const void* sum
         CombineBackParams p;
         p.dres = dresidual; p.dx = static_cast<const __nv_bfloat16*>(dx); p.sum = static_cast<const __nv_bfloat16*>(sum); p.res = residual_out;
         p.w_post = w_post; p.scale = scale; p.w_pre = w_pre;
-        p.eps = eps; p.inv_h = 1.f / (float)h; p.T = T; p.h = h;
+        p.eps = dx ? eps : fmaxf(eps, 1e-37f);                        // (without dx the next norm's terms have to be zeros, not 0 / 0)
+        p.inv_h = 1.f / (float)h; p.T = T; p.h = h;
         p.out_dres = out_dresidual; p.out_dsum = static_cast<__nv_bfloat16*>(out_dsum);
         p.parts = static_cast<float*>(workspace); p.want_parts = columns;
         p.status = ctx->status;

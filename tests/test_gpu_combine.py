@@ -89,6 +89,20 @@ def test_forward_without(T, h, k, have):
         ref.within(got.x, x, tx, "x")
 
 
+@pytest.mark.parametrize("T,h,k", [(30000, 4096, 1), (30000, 1024, 2), (9000, 8192, 1)])
+def test_residual_and_sum_do_not_depend_on_the_next_norm(T, h, k):
+    """Without the next block's norm a CTA goes from token to token with a sum over the row less."""
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(T)
+    Y, gate, res = randn(gen, T * k, h).bfloat16(), randn(gen, T, k).softmax(-1), randn(gen, T, h).bfloat16()
+    Y *= torch.exp2(torch.randint(-9, 9, (T, 1, 1), generator=gen, device="cuda").float()).expand(T, k, 1).reshape(T * k, 1).bfloat16()
+    w_post, scale, w_pre = weights(gen, h)
+    full = binding.combine(Y, gate, res, w_post, scale, w_pre, eps=EPS, want_sum=True)
+    for _ in range(5):
+        got = binding.combine(Y, gate, res, w_post, scale, None, eps=EPS, want_sum=True)
+        assert got.x is None and torch.equal(got.residual, full.residual) and torch.equal(got.sum, full.sum)
+
+
 def test_slots_with_a_gate_of_zero_are_not_read():
     T, h, k = 40, 512, 4
     gen = torch.Generator(device="cuda")
@@ -238,6 +252,18 @@ def test_in_place_and_guards(T):
     assert torch.equal(stream, first.dresidual) and torch.equal(dsum, first.dsum)
     assert all(torch.equal(a, b) for a, b in zip(grads, (first.dw_post, first.dscale, first.dw_pre)))
     assert (whole[:32] == 3).all() and (whole[-32:] == 3).all() and (ws[need:] == 0x5A).all()
+
+
+@pytest.mark.parametrize("T", [5, 1400])
+def test_no_gradient_of_the_next_norm_and_no_epsilon(T):
+    """Where dx is left out nothing of the next norm is worked out, so that an epsilon of zero does no harm."""
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(T)
+    dres, y = randn(gen, T, 264).bfloat16(), randn(gen, T, 264).bfloat16()
+    got = binding.combine_backward(dres, None, y, None, *weights(gen, 264)[:2], None, eps=0.0)
+    again = binding.combine_backward(dres, None, y, None, *weights(gen, 264)[:2], None, eps=1e-12)
+    assert torch.equal(got.dresidual, dres) and torch.isfinite(got.dsum).all() and torch.isfinite(got.dscale).all()
+    assert torch.equal(again.dresidual, dres)
 
 
 def test_no_tokens():
