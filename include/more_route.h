@@ -289,7 +289,7 @@ int more_experts_backward(const void* X, const void* W1, const void* W2, const i
  *     rms(v) = sqrt(mean(v^2) + eps)
  *
  *   Y          device bf16 [T*k][h], or NULL: nothing to join, r' = residual (the first block's norm).  A dense block's output is
- *              k = 1.  A slot whose gate is 0 adds nothing and its row is not read.
+ *              k = 1.  A slot whose gate is 0 adds nothing, whatever its row holds.
  *   gate       device fp32 [T][k], or NULL: ones.
  *   residual   device [T][h] of residual_type, or NULL: zeros (not both Y and residual).
  *   w_post, scale, w_pre   device fp32 [h], or NULL: no norm behind the block; no scale; no norm in front of the next.
