@@ -36,7 +36,7 @@ namespace {
 // two warps share a stage, and it is there sooner: 58 us instead of 62 for 3001 x 6 pairs of 504 experts, h = 1000, s = 40, 265
 // instead of 279 for 32768 x 8 of 256, h = 512, s = 256, nothing lost elsewhere.  (The backward one was 20 to 50 us slower for
 // 65536 x 4 of 8192, whose stages are small: every loader goes through all stages' places.)
-constexpr int kLoaders = 5, kFewLoaders = 3;         // where rows are gathered; elsewhere
+constexpr int kLoaders = 5, kWLoaders = 7, kFewLoaders = 3;      // where rows are gathered; for the weights' gradients; elsewhere
 __host__ __device__ constexpr int team_of(int mode) { return mode == 0 /* kUp */ ? 2 : 1; }   // warps that share a stage
 constexpr int threads_of(int loaders) { return (9 + loaders) * 32; }
 constexpr int rows_threads(int mode) { return threads_of((mode == 0 || mode == 2 ? kLoaders : kFewLoaders) * team_of(mode)); }
@@ -862,7 +862,7 @@ struct Units {
     }
 };
 
-__global__ void __launch_bounds__(threads_of(kLoaders), 1)
+__global__ void __launch_bounds__(threads_of(kWLoaders), 1)
 weights_kernel(const __grid_constant__ WeightsMaps m0, const __grid_constant__ WeightsMaps m1, const __grid_constant__ WeightsParams all)
 {
     extern __shared__ uint8_t smem_raw[];
@@ -879,7 +879,8 @@ weights_kernel(const __grid_constant__ WeightsMaps m0, const __grid_constant__ W
         // A stage is up to 64 rows, as many whole MMA steps of 16 as it needs, of both operands' boxes of 64 columns: rows by token by
         // gathers, consecutive places in pieces of 16.  Rows behind the run's last are out of bounds, zeros: of the places, too,
         // only then row by row (what lies there belongs to another expert).
-        // A loader issues a stage of its own when it has come to the next one, whose pairs it has just requested.
+        // A loader issues a stage of its own when it has come to the next one, whose pairs it has just requested.  Issuing one (16
+        // gathers, 4 boxes) takes it about 4700 clocks, passing a unit 750: with five they were what a unit waited for.
         const int loader = loader_of(warp);
         int4* rows = ctl->rows[loader];                             // 64 tokens, 64 places
         const uint64_t again = comes_again();
@@ -934,7 +935,7 @@ weights_kernel(const __grid_constant__ WeightsMaps m0, const __grid_constant__ W
                 const int left = min(64, u.n - at);
                 uint32_t where;
                 int last;
-                if (!rg.mine((uint32_t)((left + 15) / 16) * 2048 * (a_boxes + nb), loader, kLoaders, lane, &where, &last)) continue;
+                if (!rg.mine((uint32_t)((left + 15) / 16) * 2048 * (a_boxes + nb), loader, kWLoaders, lane, &where, &last)) continue;
                 int pair[2];
 #pragma unroll
                 for (int i = 0; i < 2; ++i) pair[i] = i * 32 + lane < left ? all.pairs[u.lo + at + i * 32 + lane] : -1;
@@ -1005,7 +1006,7 @@ weights_kernel(const __grid_constant__ WeightsMaps m0, const __grid_constant__ W
             const uint32_t acc = tmem + buf * 256 + ((uint32_t)(quarter * 32) << 16), to = staging + (p.by_halves() ? (it & 1) * (kXStaging / 2) : 0);
             const bool ok = mbar_wait(smem_u32(&ctl->acc_full[buf]), (it >> 1) & 1, abort_flag, all.status);   // (given up: goes on without work)
             tc_fence_after();
-            if (warp == 2) halves && p.by_halves() ? bulk_read_done<1>() : bulk_read_done<0>();
+            if (warp < 6) halves && p.by_halves() ? bulk_read_done<1>() : bulk_read_done<0>();
             halves = p.by_halves();
             epilogue_sync();
             for (int c = copy * 32; ok && c < per && row0 < rows && c0 + side * per + c < p.cols; c += copies * 32) {
@@ -1025,12 +1026,16 @@ weights_kernel(const __grid_constant__ WeightsMaps m0, const __grid_constant__ W
             ++it;
             fence_async_smem();
             epilogue_sync();
-            if (warp == 2) {
-                for (int b = 0; ok && b < p.nb && c0 + b * 64 < p.cols; ++b) tma_store_3d_elect(w.which ? &m1.out : &m0.out, to + b * box, c0 + b * 64, mt * 128, w.e, once);
+            // A box for each of four warps where two units' boxes fit: issuing a store takes about 200 clocks (65536 x 4 pairs of 8192
+            // experts, h = 512, s = 64, with seven loaders: the backward pass 825 us instead of 853); else all of them for one (of 2048
+            // experts, h = 1024, s = 128, two slots: 929 us instead of 962).
+            if (warp < 6) {
+                for (int b = warp - 2; ok && b < p.nb && c0 + b * 64 < p.cols && (p.by_halves() ? b == warp - 2 : warp == 2); ++b)
+                    tma_store_3d_elect(w.which ? &m1.out : &m0.out, to + b * box, c0 + b * 64, mt * 128, w.e, once);
                 bulk_commit();
             }
         }
-        if (warp == 2) bulk_all_done();
+        if (warp < 6) bulk_all_done();
     }
     close_cta(ctl, tmem, warp);
 }
@@ -1205,7 +1210,7 @@ int launch_weights(const ExpertsArgs& a, const Workspace& w, const DeviceCtx& ct
     p.units = (unsigned)units;
     if (allow_smem(weights_kernel) != MORE_OK) return MORE_ERR_CUDA;
     const int grid = units < ctx.sm_count ? (int)units : ctx.sm_count;
-    if (launch_behind(weights_kernel, grid, threads_of(kLoaders), kXSmem, a.stream, m[0], m[1], p) != cudaSuccess) return MORE_ERR_CUDA;
+    if (launch_behind(weights_kernel, grid, threads_of(kWLoaders), kXSmem, a.stream, m[0], m[1], p) != cudaSuccess) return MORE_ERR_CUDA;
     count_launch(1);
     return MORE_OK;
 }
