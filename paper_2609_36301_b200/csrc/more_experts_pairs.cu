@@ -4,7 +4,9 @@
 // A cluster of CTAs serves a pair.  Each takes a slice of the hidden dimension, in both products: its rows of W1 (one contiguous
 // piece of memory) give a part of every activation's sum, which the CTAs exchange through distributed shared memory (2 s floats
 // each); then its columns of W2 give its columns of the output, without a second exchange.  The first rows of W2 are requested
-// before the exchange, so that a call waits for memory about once.  Sums and the activation stay in 32 bits.
+// before the exchange, so that a call waits for memory about once.  Sums and the activation stay in 32 bits.  Bound by latency for few
+// pairs (8 of h = 2048, s = 64: 8.9 us, 6.3 MB), by the weights' bytes for many (512: 391 MB in 73 us, 5.4 TB/s).  (Requesting the first
+// rows of W2 already in front of the first product's sums: 77 us for 512 pairs, 17 instead of 16 for 64.)
 #include "more_experts.cuh"
 
 namespace more {

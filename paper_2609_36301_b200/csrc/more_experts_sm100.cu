@@ -15,14 +15,19 @@
 //   weights_kernel      dW of one expert: 128 x 256 outputs, contracted over the expert's pairs 64 at a time, both operands
 //                       MN-major.
 //
-// Rows that are anywhere in X or d come by gathering TMA loads, four rows of 128 bytes each, in the swizzled layout that the MMAs read;
-// four warps share them, as each costs its warp about 100 clocks.  (Asynchronous 16-byte copies by threads were slower: 144 us
-// against 105 for the first product of 16384 x 8 pairs, h = 512, 4096 experts of s = 64.)
+// Rows that are anywhere in X or d come by gathering TMA loads, four rows of 128 bytes each, in the swizzled layout that the MMAs read.
+// One costs the warp that issues it 100 to 200 clocks, so several warps share them.  (Asynchronous 16-byte copies by threads were
+// slower: 144 us against 105 for the first product of 16384 x 8 pairs, h = 512, 4096 experts of s = 64.)
 //
 // What bounds them: with the paper's narrow experts, the bytes: each expert's weights are read once (six bytes per h s) for as
 // few as 30 tokens.  A stage of the ring in shared memory is as long as what it holds, so that tiles of few rows have more
 // weights in flight, and gradients of weights leave shared memory by TMA stores that nobody waits for.  The activation goes
-// to the second product as bf16 rows in expert order (s of them against h of an output row).
+// to the second product as bf16 rows in expert order (s of them against h of an output row).  Measured (DRAM bytes and time of one
+// launch, cold): 16384 x 8 pairs of 4096 experts, h = 512, s = 64: kUp 560 MB in 97 us, kDown 360 MB in 72 us; 32768 x 4 of the same:
+// kBackAct 363 MB in 85 us, kBackX 688 MB in 115 us, the gradients of both weights 872 MB in 205 us, where issuing loads and passing
+// tiles through shared memory take as long as an SM's stores.  Few wide experts are bound by what the SMs read from L2: 32768 x 8
+// pairs of 256 experts, h = 512, s = 256, kUp 160 us, of which the MMAs alone take 82 (a third of the bytes would go with CTA
+// pairs that share the weights' tiles), kDown 103 us.
 #include "more_experts.cuh"
 
 #include <math.h>
@@ -153,7 +158,7 @@ struct Control {
     float gate[kTileRows];
     int4 rows[2 * kLoaders][kTileRows / 4];   // of each loader's tile
 };
-static_assert(sizeof(Control) <= kXControl, "control block");
+static_assert(sizeof(Control) <= kXControl && kWLoaders <= 2 * kLoaders, "control block");
 
 // The ring of stages, each as long as what it holds (a multiple of 1024 bytes).  Every loader, and the warp that empties it, goes
 // through the same sequence of lengths and so knows where each stage lies.
