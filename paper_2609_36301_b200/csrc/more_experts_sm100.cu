@@ -24,10 +24,10 @@
 // weights in flight, and gradients of weights leave shared memory by TMA stores that nobody waits for.  The activation goes
 // to the second product as bf16 rows in expert order (s of them against h of an output row).  Measured (DRAM bytes and time of one
 // launch, cold): 16384 x 8 pairs of 4096 experts, h = 512, s = 64: kUp 560 MB in 97 us, kDown 360 MB in 72 us; 32768 x 4 of the same:
-// kBackAct 363 MB in 85 us, kBackX 688 MB in 115 us, the gradients of both weights 872 MB in 205 us, where issuing loads and passing
+// kBackAct 363 MB in 85 us, kBackX 688 MB in 115 us, the gradients of both weights 872 MB in 193 us, where issuing loads and passing
 // tiles through shared memory take as long as an SM's stores.  Few wide experts are bound by what the SMs read from L2: 32768 x 8
-// pairs of 256 experts, h = 512, s = 256, kUp 160 us, of which the MMAs alone take 82 (a third of the bytes would go with CTA
-// pairs that share the weights' tiles), kDown 103 us.
+// pairs of 256 experts, h = 512, s = 256, kUp 160 us, of which the MMAs alone take 82 and the gathers alone 150 (about 10 clocks per
+// row of 128 bytes), kDown 103 us.
 #include "more_experts.cuh"
 
 #include <math.h>
