@@ -40,18 +40,21 @@ namespace {
 // opening a stage and issuing its loads costs a warp 700 to 3000 clocks, several times what a stage may take.  In the forward gather
 // two warps share a stage, and it is there sooner: 58 us instead of 62 for 3001 x 6 pairs of 504 experts, h = 1000, s = 40, 265
 // instead of 279 for 32768 x 8 of 256, h = 512, s = 256, nothing lost elsewhere.  (The backward one was 20 to 50 us slower for
-// 65536 x 4 of 8192, whose stages are small: every loader goes through all stages' places.)
-constexpr int kLoaders = 5, kWLoaders = 7, kFewLoaders = 3;      // where rows are gathered; for the weights' gradients; elsewhere
-__host__ __device__ constexpr int team_of(int mode) { return mode == 0 /* kUp */ ? 2 : 1; }   // warps that share a stage
+// 65536 x 4 of 8192, whose stages are small: every loader goes through all stages' places.  Seven loaders there, and for the weights'
+// gradients: 500 us instead of 510 with five for the backward pass of 8192 x 4 pairs of 64 experts, h = 4096, s = 256.)
+constexpr int kTeams = 5, kTeam = 2;                 // kUp: stages are taken by teams of two
+constexpr int kBackLoaders = 7, kFewLoaders = 3;     // where rows are gathered on the way back; where none are
 constexpr int threads_of(int loaders) { return (9 + loaders) * 32; }
-constexpr int rows_threads(int mode) { return threads_of((mode == 0 || mode == 2 ? kLoaders : kFewLoaders) * team_of(mode)); }
+__host__ __device__ constexpr int team_of(int mode) { return mode == 0 /* kUp */ ? kTeam : 1; }
+__host__ __device__ constexpr int takers_of(int mode) { return mode == 0 ? kTeams : mode == 2 /* kBackAct */ ? kBackLoaders : kFewLoaders; }
+constexpr int rows_threads(int mode) { return threads_of(takers_of(mode) * team_of(mode)); }
 __device__ __forceinline__ int loader_of(int warp) { return warp == 0 ? 0 : warp - 9; }
 constexpr int kTileRows = 128;
 constexpr int kBox = 64 * 128;                       // 64 rows of 64 bf16
 constexpr int kRowPitch = 528;                       // a staged output row: 256 16-bit values, and 16 bytes so that rows fall on other banks
 constexpr int kXStaging = kTileRows * kRowPitch;     // what the epilogue passes from the tensor memory's layout to memory's
 constexpr int kXRing = 153 * 1024;
-constexpr int kXControl = 1536 + 2 * kLoaders * 512;
+constexpr int kXControl = 1536 + kTeams * kTeam * 512;
 constexpr int kXSmem = kXRing + kXStaging + 1024 /*alignment*/ + kXControl;
 static_assert(kXSmem <= 227 * 1024, "shared memory");
 static_assert(kXStaging >= kTileRows * 128, "an operand of fewer rows than the MMA's 128 is read past its end");
@@ -156,9 +159,9 @@ struct Control {
     int abort;
     int pair[kTileRows];
     float gate[kTileRows];
-    int4 rows[2 * kLoaders][kTileRows / 4];   // of each loader's tile
+    int4 rows[kTeams * kTeam][kTileRows / 4];   // of each loader's tile
 };
-static_assert(sizeof(Control) <= kXControl && kWLoaders <= 2 * kLoaders, "control block");
+static_assert(sizeof(Control) <= kXControl && kBackLoaders <= kTeams * kTeam, "control block");
 
 // The ring of stages, each as long as what it holds (a multiple of 1024 bytes).  Every loader, and the warp that empties it, goes
 // through the same sequence of lengths and so knows where each stage lies.
@@ -479,7 +482,7 @@ rows_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUte
     const int units = p.tiles[0].x * p.chunks;
 
     if (warp == 0 || warp >= 10) {
-        constexpr int kMine = kGather ? kLoaders : kFewLoaders, kMembers = team_of(MODE);
+        constexpr int kMine = takers_of(MODE), kMembers = team_of(MODE);
         const int loader = loader_of(warp) / kMembers, member = loader_of(warp) % kMembers;
         int4* rows = ctl->rows[loader_of(warp)];
         const uint64_t again = comes_again(), once = p.weights_once ? passes_once() : comes_normally();
@@ -867,7 +870,7 @@ struct Units {
     }
 };
 
-__global__ void __launch_bounds__(threads_of(kWLoaders), 1)
+__global__ void __launch_bounds__(threads_of(kBackLoaders), 1)
 weights_kernel(const __grid_constant__ WeightsMaps m0, const __grid_constant__ WeightsMaps m1, const __grid_constant__ WeightsParams all)
 {
     extern __shared__ uint8_t smem_raw[];
@@ -940,7 +943,7 @@ weights_kernel(const __grid_constant__ WeightsMaps m0, const __grid_constant__ W
                 const int left = min(64, u.n - at);
                 uint32_t where;
                 int last;
-                if (!rg.mine((uint32_t)((left + 15) / 16) * 2048 * (a_boxes + nb), loader, kWLoaders, lane, &where, &last)) continue;
+                if (!rg.mine((uint32_t)((left + 15) / 16) * 2048 * (a_boxes + nb), loader, kBackLoaders, lane, &where, &last)) continue;
                 int pair[2];
 #pragma unroll
                 for (int i = 0; i < 2; ++i) pair[i] = i * 32 + lane < left ? all.pairs[u.lo + at + i * 32 + lane] : -1;
@@ -1215,7 +1218,7 @@ int launch_weights(const ExpertsArgs& a, const Workspace& w, const DeviceCtx& ct
     p.units = (unsigned)units;
     if (allow_smem(weights_kernel) != MORE_OK) return MORE_ERR_CUDA;
     const int grid = units < ctx.sm_count ? (int)units : ctx.sm_count;
-    if (launch_behind(weights_kernel, grid, threads_of(kWLoaders), kXSmem, a.stream, m[0], m[1], p) != cudaSuccess) return MORE_ERR_CUDA;
+    if (launch_behind(weights_kernel, grid, threads_of(kBackLoaders), kXSmem, a.stream, m[0], m[1], p) != cudaSuccess) return MORE_ERR_CUDA;
     count_launch(1);
     return MORE_OK;
 }
