@@ -5,8 +5,8 @@
 // piece of memory) give a part of every activation's sum, which the CTAs exchange through distributed shared memory (2 s floats
 // each); then its columns of W2 give its columns of the output, without a second exchange.  The first rows of W2 are requested
 // before the exchange, so that a call waits for memory about once.  Sums and the activation stay in 32 bits.  Bound by latency for few
-// pairs (8 of h = 2048, s = 64: 8.9 us, 6.3 MB), by the weights' bytes for many (512: 391 MB in 73 us, 5.4 TB/s).  (Requesting the first
-// rows of W2 already in front of the first product's sums: 77 us for 512 pairs, 17 instead of 16 for 64.)
+// pairs (8 of h = 2048, s = 64: 8.9 us, 6.3 MB), by the weights' bytes for many (512: 391 MB in 70 us, 5.6 TB/s).  (Requesting the first
+// rows of W2 already in front of the first product's sums: 4 us more for 512 pairs, 1 for 64.)
 #include "more_experts.cuh"
 
 namespace more {
@@ -41,7 +41,7 @@ __device__ __forceinline__ uint4 ld_stream(const __nv_bfloat16* p)      // weigh
 }
 
 // Threads as `groups` column groups of 8 times as many row groups as fit: acc = sum over this thread's rows of x[row] W[row][8 columns].
-template <int kBatch>                             // 16-byte loads in flight per thread, twice
+template <int kBatch, bool kTwo>                  // 16-byte loads in flight per thread, twice; kTwo: as long as there are any
 struct Slice {
     const __nv_bfloat16* at;      // of this thread's first row, or nullptr
     size_t step;                  // elements between its rows
@@ -60,16 +60,30 @@ struct Slice {
             if (at && r < rows) fma8(acc, x[r], w[i]);
         }
     }
-    __device__ void sum(float (&acc)[8], uint4 (&w)[kBatch], const float* x) const      // w: the first batch, loaded
+    // w: the first batch, loaded; v: with kTwo the second
+    __device__ void sum(float (&acc)[8], uint4 (&w)[kBatch], uint4 (&v)[kBatch], const float* x) const
     {
         const int mine = at && row < rows ? (rows - row + stride - 1) / stride : 0;
-        for (int i = 0; i < mine; i += kBatch) {
-            uint4 next[kBatch];
-            if (i + kBatch < mine) load(next, i + kBatch);
-            add(acc, w, x, i);
+        if constexpr (kTwo) {
+            for (int i = 0; i < mine; i += 2 * kBatch) {
+                add(acc, w, x, i);
+                if (i + 2 * kBatch < mine) load(w, i + 2 * kBatch);
+                if (i + kBatch < mine) add(acc, v, x, i + kBatch);
+                if (i + 3 * kBatch < mine) load(v, i + 3 * kBatch);
+            }
+        } else {
+            for (int i = 0; i < mine; i += kBatch) {
+                if (i + kBatch < mine) load(v, i + kBatch);
+                add(acc, w, x, i);
 #pragma unroll
-            for (int j = 0; j < kBatch; ++j) w[j] = next[j];
+                for (int j = 0; j < kBatch; ++j) w[j] = v[j];
+            }
         }
+    }
+    __device__ void begin(uint4 (&w)[kBatch], uint4 (&v)[kBatch]) const
+    {
+        load(w, 0);
+        if constexpr (kTwo) load(v, kBatch);
     }
 };
 
@@ -84,8 +98,10 @@ __device__ __forceinline__ float column_sum(const float* red, int cols, int row_
     return (v[0] + v[1]) + (v[2] + v[3]);
 }
 
-// BATCH, PER_SM: what a CTA has in flight, and how many of them are resident.
-template <int BATCH, int PER_SM>
+// BATCH, PER_SM: what a CTA has in flight, and how many of them are resident.  TWO: two batches are in flight all the time, in twice the
+// code: 512 pairs of h = 2048, s = 64 70 us instead of 73, 128 of h = 4096, s = 128 76.5 instead of 80.3; but 8 pairs, which run their
+// code once, 9.2 instead of 8.9.
+template <int BATCH, int PER_SM, bool TWO>
 __global__ void __launch_bounds__(kPThreads, PER_SM)
 pairs_kernel(const __nv_bfloat16* __restrict__ X, const __nv_bfloat16* __restrict__ W1, const __nv_bfloat16* __restrict__ W2,
              const int32_t* __restrict__ idx, int h, int s, int M, int k, int ranks, __nv_bfloat16* __restrict__ Y)
@@ -104,19 +120,19 @@ pairs_kernel(const __nv_bfloat16* __restrict__ X, const __nv_bfloat16* __restric
     // first product: columns in passes of up to 256 groups of 8
     const __nv_bfloat16* w1 = W1 + ((size_t)e * h + v0 * 8) * 2 * s;
     const int all = s / 4;
-    uint4 w[BATCH];
+    uint4 w[BATCH], v[BATCH];
     for (int g0 = 0; g0 < all; g0 += kPThreads) {
         const int groups = min(all - g0, kPThreads), rg = kPThreads / groups;
         const int mine = tid / groups, col = (g0 + tid % groups) * 8;
-        Slice<BATCH> sl{mine < rg ? w1 + (size_t)mine * 2 * s + col : nullptr, (size_t)rg * 2 * s, rows, mine, rg};
-        sl.load(w, 0);
+        Slice<BATCH, TWO> sl{mine < rg ? w1 + (size_t)mine * 2 * s + col : nullptr, (size_t)rg * 2 * s, rows, mine, rg};
+        sl.begin(w, v);
         if (g0 == 0) {
             const __nv_bfloat16* from = X + (size_t)(pair / k) * h + v0 * 8;
             for (int i = tid; i < rows; i += kPThreads) x[i] = __bfloat162float(from[i]);
             __syncthreads();
         }
         float acc[8] = {};
-        sl.sum(acc, w, x);
+        sl.sum(acc, w, v, x);
         if (mine < rg)
 #pragma unroll
             for (int i = 0; i < 8; ++i) red[mine * groups * 8 + (tid % groups) * 8 + i] = acc[i];
@@ -130,9 +146,9 @@ pairs_kernel(const __nv_bfloat16* __restrict__ X, const __nv_bfloat16* __restric
     auto slice2 = [&](int g0) {
         const int groups = min(vn - g0, kPThreads), rg = groups > 0 ? kPThreads / groups : 0;
         const int mine = groups > 0 ? tid / groups : 0;
-        return Slice<BATCH>{mine < rg ? W2 + ((size_t)e * s + mine) * h + (size_t)(v0 + g0 + tid % groups) * 8 : nullptr, (size_t)rg * h, s, mine, rg};
+        return Slice<BATCH, TWO>{mine < rg ? W2 + ((size_t)e * s + mine) * h + (size_t)(v0 + g0 + tid % groups) * 8 : nullptr, (size_t)rg * h, s, mine, rg};
     };
-    if (passes > 0) slice2(0).load(w, 0);
+    if (passes > 0) slice2(0).begin(w, v);
     cluster_wait();
     const uint32_t part_at = smem_u32(part);
     for (int c = tid; c < s; c += kPThreads) {
@@ -153,10 +169,10 @@ pairs_kernel(const __nv_bfloat16* __restrict__ X, const __nv_bfloat16* __restric
     cluster_arrive();                                  // (done with the other CTAs' parts)
     for (int p = 0; p < passes; ++p) {
         const int g0 = p * kPThreads, groups = min(vn - g0, kPThreads), rg = kPThreads / groups;
-        const Slice<BATCH> sl = slice2(g0);
-        if (p > 0) sl.load(w, 0);
+        const Slice<BATCH, TWO> sl = slice2(g0);
+        if (p > 0) sl.begin(w, v);
         float acc[8] = {};
-        sl.sum(acc, w, act);
+        sl.sum(acc, w, v, act);
         if (tid / groups < rg)
 #pragma unroll
             for (int i = 0; i < 8; ++i) red[(tid / groups) * groups * 8 + (tid % groups) * 8 + i] = acc[i];
@@ -183,7 +199,9 @@ int launch_experts_pairs(const ExpertsArgs& a, const DeviceCtx& ctx)
     // More pairs than two CTAs per SM hold at once: four smaller ones (512 pairs of h = 2048, s = 64: 72 us instead of 90; for fewer
     // pairs they are slower, 8: 11.3 instead of 9.2, 128 of h = 4096, s = 128: 108 instead of 84).
     const bool many = P > 2LL * ctx.sm_count;
-    auto kern = many ? pairs_kernel<4, 4> : pairs_kernel<8, 2>;
+    // (eight batches of W1 per thread or more: 256 pairs of h = 1024, s = 32, which have four, 16.2 instead of 14.6)
+    const bool two = (long long)(a.h / ranks) * (a.s / 4) >= 64LL * kPThreads;
+    auto kern = many ? pairs_kernel<4, 4, true> : two ? pairs_kernel<8, 2, true> : pairs_kernel<8, 2, false>;
     if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return MORE_ERR_CUDA;
     if (P * ranks > 0x7fffffffLL) return MORE_ERR_TOO_LARGE;
     cudaLaunchConfig_t cfg{};
