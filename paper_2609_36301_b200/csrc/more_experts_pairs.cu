@@ -72,11 +72,13 @@ struct Slice {
                 if (i + 3 * kBatch < mine) load(v, i + 3 * kBatch);
             }
         } else {
+            uint4 here[kBatch];
+            uint4 (&next)[kBatch] = kBatch > 4 ? v : here;   // (v lives on between the sums, for which 64 registers are too few)
             for (int i = 0; i < mine; i += kBatch) {
-                if (i + kBatch < mine) load(v, i + kBatch);
+                if (i + kBatch < mine) load(next, i + kBatch);
                 add(acc, w, x, i);
 #pragma unroll
-                for (int j = 0; j < kBatch; ++j) w[j] = v[j];
+                for (int j = 0; j < kBatch; ++j) w[j] = next[j];
             }
         }
     }
@@ -197,11 +199,12 @@ int launch_experts_pairs(const ExpertsArgs& a, const DeviceCtx& ctx)
     while (ranks < 8 && P * ranks * 2 <= 2LL * ctx.sm_count && a.h / (ranks * 2) >= 32) ranks *= 2;
     const size_t smem = sizeof(float) * (kPThreads * 8 + 3 * (size_t)a.s + ((size_t)a.h / 8 + ranks - 1) / ranks * 8);
     // More pairs than two CTAs per SM hold at once: four smaller ones (512 pairs of h = 2048, s = 64: 72 us instead of 90; for fewer
-    // pairs they are slower, 8: 11.3 instead of 9.2, 128 of h = 4096, s = 128: 108 instead of 84).
+    // pairs they are slower, 8: 11.3 instead of 9.2, 128 of h = 4096, s = 128: 108 instead of 84).  TWO where a thread has batches enough
+    // for it (4096 pairs of h = 256, s = 16, one each: 70 us without, 76 with; 16 of h = 4096, s = 128, eight each: 19.7 and 22).
     const bool many = P > 2LL * ctx.sm_count;
-    // (eight batches of W1 per thread or more: 256 pairs of h = 1024, s = 32, which have four, 16.2 instead of 14.6)
-    const bool two = (long long)(a.h / ranks) * (a.s / 4) >= 64LL * kPThreads;
-    auto kern = many ? pairs_kernel<4, 4, true> : two ? pairs_kernel<8, 2, true> : pairs_kernel<8, 2, false>;
+    const long long per_thread = (long long)(a.h / ranks) * (a.s / 4) / kPThreads;         // rows of W1
+    auto kern = many ? (per_thread >= 32 ? pairs_kernel<4, 4, true> : pairs_kernel<4, 4, false>)
+                     : (per_thread >= 128 ? pairs_kernel<8, 2, true> : pairs_kernel<8, 2, false>);
     if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return MORE_ERR_CUDA;
     if (P * ranks > 0x7fffffffLL) return MORE_ERR_TOO_LARGE;
     cudaLaunchConfig_t cfg{};
