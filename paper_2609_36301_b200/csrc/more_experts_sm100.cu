@@ -1320,23 +1320,24 @@ int check_sizes(int T, int h, int s, int M, int k)
     return MORE_OK;
 }
 
-// Which forward path.  Pairs read their expert's weights each, 8 us behind a start (20 GB/s per CTA, 6.2 TB/s in all).  Tiles read those
-// of the experts that are hit, of evenly spread ids M (1 - exp(-P / M)), 24 us behind for three kernels; a kernel takes the bytes'
-// time (100 GB/s per unit, 6.2 TB/s in all) or that of its stages, 0.35 us each of the first, 0.8 of the second, over the SMs.
-// Measured on eight combinations of h, s and M from 8 to 8192 pairs (us, pairs / tiles): h = 2048, s = 64, M = 8192: 12 / 31 at 8
-// pairs, 76 / 84 at 512, 141 / 135 at 1024, 266 / 231 at 2048; h = 512, s = 64, M = 64: 14 / 25 at 128, 25 / 25 at 512, 41 / 25
-// at 1024; h = 4096, s = 512, M = 16: 72 / 51 at 8.  The choice cost 4 % at worst there.
+// Which forward path.  Pairs read their expert's weights each, 9 us behind a start (20 GB/s per CTA, 6.2 TB/s in all), 0.016 us per pair at
+// least.  Tiles read those of the experts that are hit, of evenly spread ids M (1 - exp(-P / M)), 20 us behind for three kernels; a
+// kernel takes the bytes' time (100 GB/s per unit, 6.2 TB/s in all) or that of its stages, 0.3 us each of the first, 0.8 of the
+// second, over the SMs.  Measured on eight combinations of h, s and M from 8 to 8192 pairs (us, pairs / tiles): h = 2048, s = 64,
+// M = 8192: 12 / 26 at 8 pairs, 74 / 80 at 512, 137 / 133 at 1024, 260 / 222 at 2048; h = 512, s = 64, M = 64: 14 / 20 at 128, 25 / 20
+// at 512, 38 / 20 at 1024; h = 256, s = 16, M = 16384: 46 / 46 at 2048, 136 / 103 at 8192; h = 4096, s = 512, M = 16: 68 / 46 at
+// 8.  The choice cost 2 % at worst in the run that it was fitted to, 7 % in the next.
 int cheaper_path(int T, int h, int s, int M, int k)
 {
     const double P = (double)T * k, weights = 6.0 * h * s, sms = 148, most = 6.2e6;     // bytes; bytes per us
     const double hit = M * -expm1(-P / M);
     double ctas = P;                                                 // as launch_experts_pairs has them
     for (int ranks = 1; ranks < 8 && ctas * 2 <= 2 * sms && h / (ranks * 2) >= 32; ranks *= 2) ctas *= 2;
-    const double pairs = 8 + P * (0.009 + weights / fmin(most, fmin(ctas, 2 * sms) * 20e3));
+    const double pairs = 9 + P * fmax(0.016, 0.008 + weights / fmin(most, fmin(ctas, 2 * sms) * 20e3));
     const double wide = (s + 127) / 128, rate = fmin(most, hit * wide * 100e3);
-    const double up = hit * fmax(weights * 2 / 3 / rate, wide * ((h + 63) / 64) * 0.35 / sms);
+    const double up = hit * fmax(weights * 2 / 3 / rate, wide * ((h + 63) / 64) * 0.3 / sms);
     const double down = hit * fmax(weights / 3 / rate, ((h + 255) / 256) * ((s + 63) / 64) * 0.8 / sms);
-    const double tiles = 24 + up + down;
+    const double tiles = 20 + up + down;
     return pairs <= tiles ? MORE_EXPERTS_PAIRS : MORE_EXPERTS_TILES;
 }
 
