@@ -617,6 +617,13 @@ int ring_stages(size_t token, int* per_sm)
     const size_t n = kRingBytesPerSm / *per_sm / token;
     return n < 2 ? 0 : n > kStages ? kStages : (int)n;
 }
+// The limit belongs to the kernel, not to a call: always the largest ring, or a call of another host thread with shorter rows, between
+// this and the launch, would have the launch refused.
+template <class Kernel>
+int allow_ring(Kernel kern)
+{
+    return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingBytesPerSm) == cudaSuccess ? MORE_OK : MORE_ERR_CUDA;
+}
 template <int NV, class R, int THREADS>
 int launch_back(CombineBackParams p, const BackPlan& b, cudaStream_t st)
 {
@@ -624,7 +631,7 @@ int launch_back(CombineBackParams p, const BackPlan& b, cudaStream_t st)
     int per_sm = b.per_sm;
     p.stages = ring_stages(token, &per_sm);                          // (two of the longest rows, 96 KB each, fit)
     const size_t smem = p.stages * token;
-    if (cudaFuncSetAttribute(combine_back_kernel<NV, R, THREADS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return MORE_ERR_CUDA;
+    if (allow_ring(combine_back_kernel<NV, R, THREADS>) != MORE_OK) return MORE_ERR_CUDA;
     combine_back_kernel<NV, R, THREADS><<<b.ctas, b.width, smem, st>>>(p);
     return MORE_OK;
 }
@@ -639,7 +646,7 @@ int launch_ring(const CombineParams& p, int* status, cudaStream_t st, bool* done
     if (!*done) return MORE_OK;
     const int ctas = p.T < 148 * per_sm ? p.T : 148 * per_sm;
     const size_t smem = stages * token;
-    if (cudaFuncSetAttribute(combine_ring_kernel<NV, R>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return MORE_ERR_CUDA;
+    if (allow_ring(combine_ring_kernel<NV, R>) != MORE_OK) return MORE_ERR_CUDA;
     combine_ring_kernel<NV, R><<<ctas, width, smem, st>>>(p, stages, status);
     return MORE_OK;
 }

@@ -188,6 +188,12 @@ pairs_kernel(const __nv_bfloat16* __restrict__ X, const __nv_bfloat16* __restric
     cluster_wait();
 }
 
+// Shared memory of a CTA: sums by thread, both projections' parts, the activation, a slice of x.
+constexpr size_t pairs_smem(int h, int s, int ranks)
+{
+    return sizeof(float) * (kPThreads * 8 + 3 * (size_t)s + ((size_t)h / 8 + ranks - 1) / ranks * 8);
+}
+
 }  // namespace
 
 int launch_experts_pairs(const ExpertsArgs& a, const DeviceCtx& ctx)
@@ -197,7 +203,7 @@ int launch_experts_pairs(const ExpertsArgs& a, const DeviceCtx& ctx)
     // with one CTA each, 9.2 with eight; 64: 38, 16.7 with four, 21 with eight; 512: 90, 96 with two, 111 with four.)
     int ranks = 1;
     while (ranks < 8 && P * ranks * 2 <= 2LL * ctx.sm_count && a.h / (ranks * 2) >= 32) ranks *= 2;
-    const size_t smem = sizeof(float) * (kPThreads * 8 + 3 * (size_t)a.s + ((size_t)a.h / 8 + ranks - 1) / ranks * 8);
+    const size_t smem = pairs_smem(a.h, a.s, ranks);
     // More pairs than two CTAs per SM hold at once: four smaller ones (512 pairs of h = 2048, s = 64: 72 us instead of 90; for fewer
     // pairs they are slower, 8: 11.3 instead of 9.2, 128 of h = 4096, s = 128: 108 instead of 84).  TWO where a thread has batches enough
     // for it (4096 pairs of h = 256, s = 16, one each: 70 us without, 76 with; 16 of h = 4096, s = 128, eight each: 19.7 and 22).
@@ -205,7 +211,11 @@ int launch_experts_pairs(const ExpertsArgs& a, const DeviceCtx& ctx)
     const long long per_thread = (long long)(a.h / ranks) * (a.s / 4) / kPThreads;         // rows of W1
     auto kern = many ? (per_thread >= 32 ? pairs_kernel<4, 4, true> : pairs_kernel<4, 4, false>)
                      : (per_thread >= 128 ? pairs_kernel<8, 2, true> : pairs_kernel<8, 2, false>);
-    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return MORE_ERR_CUDA;
+    // (always the most that any call needs: the limit belongs to the kernel, and a call of another host thread with narrower experts,
+    // between this and the launch, would have the launch refused)
+    constexpr size_t kMost = pairs_smem(MORE_H_MAX, MORE_S_MAX, 1);
+    static_assert(kMost <= 227 * 1024, "shared memory");
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMost) != cudaSuccess) return MORE_ERR_CUDA;
     if (P * ranks > 0x7fffffffLL) return MORE_ERR_TOO_LARGE;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(P * ranks));
