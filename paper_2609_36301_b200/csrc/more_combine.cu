@@ -313,7 +313,7 @@ __global__ void __launch_bounds__(512) combine_ring_kernel(const __grid_constant
     for (long long t = blockIdx.x; t < p.T; t += gridDim.x) {
         const float gates = next_gate;
         next_gate = gate_of(t + gridDim.x);
-        const bool ok = mbar_wait(smem_u32(&full[stage]), phase, abort_flag, status);    // (given up: goes on, the outputs are undefined)
+        const bool ok = mbar_wait_warp(smem_u32(&full[stage]), phase, abort_flag, status);    // (given up: goes on, the outputs are undefined)
         const uint8_t* from = ring + stage * bytes;
         uint64_t y[NV][4], r[NV][4];
 #pragma unroll
@@ -452,7 +452,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) combine_back_
     int stage = 0;
     uint32_t phase = 0;
     for (long long t = blockIdx.x; t < p.T; t += gridDim.x) {
-        const bool ok = mbar_wait(smem_u32(&full[stage]), phase, abort_flag, p.status);   // (given up: goes on, the outputs are undefined)
+        const bool ok = mbar_wait_warp(smem_u32(&full[stage]), phase, abort_flag, p.status);   // (given up: goes on, the outputs are undefined)
         const uint8_t* from = ring + stage * bytes;
         uint64_t g[NV][4], r[NV][4], v[NV][4], d[NV][4], y[NV][4];
         float q[3] = {0.f, 0.f, 0.f};                        // sums of r^2, r v, y^2

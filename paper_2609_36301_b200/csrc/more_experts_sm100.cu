@@ -201,7 +201,7 @@ struct Ring {
     {
         int last;
         if (!mine(bytes, loader, loaders, lane, at, &last)) return false;
-        if (last >= 0 && !mbar_wait(smem_u32(&c->empty[last % kSlots]), (last / kSlots) & 1, abort_flag, status)) *live = false;
+        if (last >= 0 && !mbar_wait_warp(smem_u32(&c->empty[last % kSlots]), (last / kSlots) & 1, abort_flag, status)) *live = false;
         __syncwarp();
         return *live;
     }
@@ -547,12 +547,12 @@ rows_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUte
                 const int in_block = MODE == kBackAct ? ks % kSumSteps : ks;
                 const uint32_t d = tmem + (it & 1) * 256;
                 if (in_block == 0) {
-                    if (!mbar_wait(smem_u32(&ctl->acc_empty[it & 1]), ((it >> 1) & 1) ^ 1u, abort_flag, p.status)) { live = false; break; }
+                    if (!mbar_wait_warp(smem_u32(&ctl->acc_empty[it & 1]), ((it >> 1) & 1) ^ 1u, abort_flag, p.status)) { live = false; break; }
                     tc_fence_after();
                 }
                 uint32_t from;
                 const uint32_t off = rg.place(steps * bytes, &from);
-                if (!mbar_wait(smem_u32(&ctl->full[rg.slot()]), rg.parity(), abort_flag, p.status)) { live = false; break; }
+                if (!mbar_wait_warp(smem_u32(&ctl->full[rg.slot()]), rg.parity(), abort_flag, p.status)) { live = false; break; }
                 tc_fence_after();
                 uint32_t al = (uint32_t)a0 + (off >> 4), bl = (uint32_t)b0 + ((off + a_bytes) >> 4);
                 for (int i = 0; i < steps; ++i, al += bytes >> 4, bl += bytes >> 4) {
@@ -580,7 +580,7 @@ rows_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUte
             const int buf = it & 1, rows = min(32, u.tile.z - r0), place0 = u.tile.y + r0;
             const uint32_t acc = tmem + buf * 256 + ((uint32_t)r0 << 16);
             const int cols = p.nb * 32, per = cols / 2, s0 = u.chunk * cols + side * per;      // s columns of the unit; of this warp
-            if (!mbar_wait(smem_u32(&ctl->acc_full[buf]), (it >> 1) & 1, abort_flag, p.status)) break;
+            if (!mbar_wait_warp(smem_u32(&ctl->acc_full[buf]), (it >> 1) & 1, abort_flag, p.status)) break;
             tc_fence_after();
             if (rows > 0 && s0 < p.s) {
                 const int limit = min(per, p.s - s0);
@@ -637,7 +637,7 @@ rows_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUte
                 const int buf = it & 1;
                 const uint32_t acc = tmem + buf * 256 + ((uint32_t)r0 << 16);
                 // after a wait that gave up the loop goes on without work: no warp is left alone at a barrier
-                ok &= mbar_wait(smem_u32(&ctl->acc_full[buf]), (it >> 1) & 1, abort_flag, p.status);
+                ok &= mbar_wait_warp(smem_u32(&ctl->acc_full[buf]), (it >> 1) & 1, abort_flag, p.status);
                 tc_fence_after();
                 if (ok && r0 < tile.z)                              // (a warp whose rows are all behind the tile adds nothing)
                     for (int pass = 0; pass < passes; ++pass) {
@@ -710,7 +710,7 @@ rows_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUte
             const int buf = it & 1, c0 = u.chunk * p.nb * 64, cols = min(p.nb * 64, p.h - c0);
             const uint32_t acc = tmem + buf * 256 + ((uint32_t)(quarter * 32) << 16);
             // (after a wait that gave up the loop goes on without work: no warp is left alone at a barrier)
-            const bool ok = mbar_wait(smem_u32(&ctl->acc_full[buf]), (it >> 1) & 1, abort_flag, p.status);
+            const bool ok = mbar_wait_warp(smem_u32(&ctl->acc_full[buf]), (it >> 1) & 1, abort_flag, p.status);
             tc_fence_after();
             const int unlike = unlike_boxes(u.tile.z), copy = quarter / unlike, pieces = u.tile.z > 64 ? 2 : 1;
             for (int q = 0; q < pieces; ++q, ++piece) {
@@ -912,7 +912,7 @@ weights_kernel(const __grid_constant__ WeightsMaps m0, const __grid_constant__ W
                 reinterpret_cast<int*>(rows)[r] = in ? all.by_k(pair) : all.T;
                 reinterpret_cast<int*>(rows)[64 + r] = in ? own.first + r : all.P;
             }
-            if (own.last >= 0 && !mbar_wait(smem_u32(&ctl->empty[own.last % kSlots]), (own.last / kSlots) & 1, abort_flag, all.status)) {
+            if (own.last >= 0 && !mbar_wait_warp(smem_u32(&ctl->empty[own.last % kSlots]), (own.last / kSlots) & 1, abort_flag, all.status)) {
                 live = false;
                 return;
             }
@@ -971,13 +971,13 @@ weights_kernel(const __grid_constant__ WeightsMaps m0, const __grid_constant__ W
             if (n == 0) continue;                                   // (the epilogue writes zeros without an accumulator)
             const int buf = it & 1, a_boxes = all.of(u.which).boxes_of_rows(u.mt), nb = all.of(u.which).nb;
             const uint32_t idesc = idesc_of(nb * 64, 1, 1);
-            if (!mbar_wait(smem_u32(&ctl->acc_empty[buf]), ((it >> 1) & 1) ^ 1u, abort_flag, all.status)) break;
+            if (!mbar_wait_warp(smem_u32(&ctl->acc_empty[buf]), ((it >> 1) & 1) ^ 1u, abort_flag, all.status)) break;
             tc_fence_after();
             for (int at = 0; at < n; at += 64) {
                 const uint32_t steps = (min(64, n - at) + 15) / 16, box = steps * 2048;
                 uint32_t from;
                 const uint32_t off = rg.place(box * (a_boxes + nb), &from);
-                if (!mbar_wait(smem_u32(&ctl->full[rg.slot()]), rg.parity(), abort_flag, all.status)) { live = false; break; }
+                if (!mbar_wait_warp(smem_u32(&ctl->full[rg.slot()]), rg.parity(), abort_flag, all.status)) { live = false; break; }
                 tc_fence_after();
                 // boxes lie `box` apart: the distance of 64 columns in both descriptors
                 const uint32_t a_lo = ((uint32_t)d0 + (off >> 4)) | (box >> 4) << 16, b_lo = a_lo + (a_boxes * box >> 4), hi = (uint32_t)(d0 >> 32);
@@ -1012,7 +1012,7 @@ weights_kernel(const __grid_constant__ WeightsMaps m0, const __grid_constant__ W
             }
             const int buf = it & 1;
             const uint32_t acc = tmem + buf * 256 + ((uint32_t)(quarter * 32) << 16), to = staging + (p.by_halves() ? (it & 1) * (kXStaging / 2) : 0);
-            const bool ok = mbar_wait(smem_u32(&ctl->acc_full[buf]), (it >> 1) & 1, abort_flag, all.status);   // (given up: goes on without work)
+            const bool ok = mbar_wait_warp(smem_u32(&ctl->acc_full[buf]), (it >> 1) & 1, abort_flag, all.status);   // (given up: goes on without work)
             tc_fence_after();
             if (warp < 6) halves && p.by_halves() ? bulk_read_done<1>() : bulk_read_done<0>();
             halves = p.by_halves();

@@ -90,6 +90,12 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
     }
     return true;
 }
+// The same for a converged warp that stays together: all of its lanes give up where one does.  (Each lane tests the barrier and its
+// budget by itself; lanes that parted here would wait for one another at the next elect, shuffle or aligned instruction for good.)
+__device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* status)
+{
+    return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, status));
+}
 
 __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1)
 {

@@ -1,0 +1,24 @@
+"""What can be held to without a GPU, from the kernels' sources: paths that a run takes only when a bounded wait gives up, and orders
+that a run keeps or breaks by the compiler's choice."""
+import os
+import re
+
+import pytest
+
+CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2609_36301_b200", "csrc")
+
+
+def source(name):
+    """A file without its comments."""
+    with open(os.path.join(CSRC, name)) as f:
+        return re.sub(r"//[^\n]*", "", f.read())
+
+
+@pytest.mark.parametrize("name", ["more_experts_sm100.cu", "more_combine.cu"])
+def test_warps_that_stay_together_give_up_together(name):
+    """All lanes of a warp wait in these kernels, and go on to instructions that need all of them."""
+    text = source(name)
+    assert len(re.findall(r"\bmbar_wait_warp\(", text)) >= 2
+    assert not re.findall(r"\bmbar_wait\(", text)
+    common = source("sm100_common.cuh")
+    assert re.search(r"bool mbar_wait_warp\([^)]*\)\s*\{\s*return __all_sync\(0xffffffffu, mbar_wait\(", common)
