@@ -61,6 +61,16 @@ __device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&v)[8])
     *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
 }
 
+// In front of the end of a CTA with a ring: where a wait gave up, copies that are still under way land before the memory is released.
+__device__ __forceinline__ void settle(volatile int* abort_flag)
+{
+    __syncthreads();
+    if (!*abort_flag) return;                        // (the same for all threads: none waits any more)
+    if (threadIdx.x == 0)
+        for (int i = 0; i < 200; ++i) __nanosleep(1000);
+    __syncthreads();
+}
+
 // Eight values as four pairs, for the instructions that work on two at a time.
 __device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b)
 {
@@ -383,6 +393,7 @@ __global__ void __launch_bounds__(512) combine_ring_kernel(const __grid_constant
             store8(p.out_x + (size_t)t * p.h + c, r[n]);
         }
     }
+    settle(abort_flag);
 }
 
 struct CombineBackParams {
@@ -527,6 +538,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) combine_back_
         }
         if (!(p.out_dsum && p.w_post)) __syncthreads();      // the next token's first sum may overwrite this one's
     }
+    settle(abort_flag);
     if (!p.want_parts) return;
     float* out = p.parts + (size_t)blockIdx.x * 2 * p.h;
 #pragma unroll

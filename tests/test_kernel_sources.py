@@ -22,3 +22,14 @@ def test_warps_that_stay_together_give_up_together(name):
     assert not re.findall(r"\bmbar_wait\(", text)
     common = source("sm100_common.cuh")
     assert re.search(r"bool mbar_wait_warp\([^)]*\)\s*\{\s*return __all_sync\(0xffffffffu, mbar_wait\(", common)
+
+
+def test_a_ring_settles_before_its_cta_ends():
+    """A CTA that gave up a wait has copies under way into its shared memory: it goes on to its end only behind a pause for them."""
+    text = source("more_combine.cu")
+    kernels = [k for k in re.split(r"__global__", text)[1:] if "mbar_wait_warp(" in k]
+    assert len(kernels) == 2
+    for k in kernels:
+        loop = k.index("mbar_wait_warp(")
+        assert "settle(abort_flag);" in k[loop:] and not re.search(r"\breturn\b", k[loop:k.index("settle(abort_flag);")])
+    assert re.search(r"void settle\([^)]*\)\s*\{\s*__syncthreads\(\);\s*if \(!\*abort_flag\) return;.*__nanosleep.*__syncthreads\(\);", text, re.S)
