@@ -551,9 +551,10 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) combine_back_
     }
 }
 
-// out = sums over the parts, in their order: 32 columns per CTA, 32 rows of threads take every 32nd part.
-__global__ void __launch_bounds__(1024) combine_columns_kernel(const float* __restrict__ parts, int count, int h, const float* __restrict__ w_post,
-                                                                const float* __restrict__ scale, float* out_dw_post, float* out_dscale, float* out_dw_pre)
+// out = sums over the parts, in their order: 32 columns per CTA, 32 rows of threads take every 32nd part.  (No promise that the parts stay
+// the same while it runs: it begins while they are being written, and a load through the read-only path could move in front of the wait.)
+__global__ void __launch_bounds__(1024) combine_columns_kernel(const float* parts, int count, int h, const float* w_post, const float* scale,
+                                                                float* out_dw_post, float* out_dscale, float* out_dw_pre)
 {
     wait_for_previous();
     __shared__ float buf[32][33];

@@ -33,3 +33,17 @@ def test_a_ring_settles_before_its_cta_ends():
         loop = k.index("mbar_wait_warp(")
         assert "settle(abort_flag);" in k[loop:] and not re.search(r"\breturn\b", k[loop:k.index("settle(abort_flag);")])
     assert re.search(r"void settle\([^)]*\)\s*\{\s*__syncthreads\(\);\s*if \(!\*abort_flag\) return;.*__nanosleep.*__syncthreads\(\);", text, re.S)
+
+
+def test_kernels_that_begin_early_promise_nothing_about_their_inputs():
+    """A kernel that may begin before the one in front of it has ended does not take what that one writes as __restrict__ (or read-only),
+    which would let its loads move in front of the wait."""
+    seen = 0
+    for name in sorted(os.listdir(CSRC)):
+        text = source(name)
+        for kernel in re.split(r"__global__", text)[1:]:
+            signature, body = kernel.split("{", 1)
+            if "wait_for_previous();" in body:
+                seen += 1
+                assert "__restrict__" not in signature and "__ldg(" not in body and "ld.global.nc" not in body, (name, signature)
+    assert seen >= 4
