@@ -64,6 +64,12 @@ constexpr int kSlots = 16;                           // stages in flight at most
 // bias towards zero, in one piece, and are as good as at h = 512, 4.7e-7, in pieces.
 constexpr int kSumSteps = 8;
 
+// Gradients of weights add up a run of pairs in pieces of this many, for the same reason: in one piece a run comes out too small by up to
+// n / 16 x 2/3 x 2^-24, and 524288 pairs of one expert did by 5.2e-4 (an eighth of bf16's half step, growing with the run); in pieces
+// it is 2e-5 at most, at any length.  And what waits for an accumulator waits for a piece, well inside its budget: a run of 4e8 pairs in
+// one piece took longer than that.  One expert, h = 512, s = 64, 65536 pairs: the backward pass 1223 us with one piece, 1243 with eight.
+constexpr int kRunPiece = 8192;
+
 enum { kUp = 0, kDown = 1, kBackAct = 2, kBackX = 3 };
 
 // Loads as a converged warp issues them: every lane passes the same operands and elect.sync picks the lane that issues.  (The
@@ -969,11 +975,14 @@ weights_kernel(const __grid_constant__ WeightsMaps m0, const __grid_constant__ W
         for (Units u(all); u.more() && live; u.next()) {
             const int n = u.n;
             if (n == 0) continue;                                   // (the epilogue writes zeros without an accumulator)
-            const int buf = it & 1, a_boxes = all.of(u.which).boxes_of_rows(u.mt), nb = all.of(u.which).nb;
+            const int a_boxes = all.of(u.which).boxes_of_rows(u.mt), nb = all.of(u.which).nb;
             const uint32_t idesc = idesc_of(nb * 64, 1, 1);
-            if (!mbar_wait_warp(smem_u32(&ctl->acc_empty[buf]), ((it >> 1) & 1) ^ 1u, abort_flag, all.status)) break;
-            tc_fence_after();
             for (int at = 0; at < n; at += 64) {
+                const int buf = it & 1, in_piece = at % kRunPiece;
+                if (in_piece == 0) {
+                    if (!mbar_wait_warp(smem_u32(&ctl->acc_empty[buf]), ((it >> 1) & 1) ^ 1u, abort_flag, all.status)) { live = false; break; }
+                    tc_fence_after();
+                }
                 const uint32_t steps = (min(64, n - at) + 15) / 16, box = steps * 2048;
                 uint32_t from;
                 const uint32_t off = rg.place(box * (a_boxes + nb), &from);
@@ -982,12 +991,14 @@ weights_kernel(const __grid_constant__ WeightsMaps m0, const __grid_constant__ W
                 // boxes lie `box` apart: the distance of 64 columns in both descriptors
                 const uint32_t a_lo = ((uint32_t)d0 + (off >> 4)) | (box >> 4) << 16, b_lo = a_lo + (a_boxes * box >> 4), hi = (uint32_t)(d0 >> 32);
                 for (uint32_t q = 0; q < steps; ++q)
-                    tc_mma_bf16_ss_elect(tmem + buf * 256, a_lo + q * 128, hi, b_lo + q * 128, hi, idesc, at > 0 || q > 0);
+                    tc_mma_bf16_ss_elect(tmem + buf * 256, a_lo + q * 128, hi, b_lo + q * 128, hi, idesc, in_piece > 0 || q > 0);
                 tc_commit_elect(smem_u32(&ctl->empty[rg.slot()]));
                 ++rg.n;
+                if (in_piece + 64 == kRunPiece || at + 64 >= n) {
+                    tc_commit_elect(smem_u32(&ctl->acc_full[buf]));
+                    ++it;
+                }
             }
-            if (live) tc_commit_elect(smem_u32(&ctl->acc_full[buf]));
-            ++it;
         }
     } else {
         // bf16 boxes of 64 columns in the layout of a swizzled TMA store, which cuts off what is behind the ends, of 128 rows, or of 64
@@ -995,6 +1006,7 @@ weights_kernel(const __grid_constant__ WeightsMaps m0, const __grid_constant__ W
         const int quarter = warp & 3, side = warp >= 6, tid = threadIdx.x - 64;
         const uint64_t once = passes_once();
         int it = 0;
+        uint32_t half = 0;                                          // of staging, where units' boxes fit one; a unit after the other
         bool halves = true;                                         // the unit before kept to its half of staging
         for (Units w(all); w.more(); w.next()) {
             const WeightsSide p = all.of(w.which);
@@ -1010,10 +1022,32 @@ weights_kernel(const __grid_constant__ WeightsMaps m0, const __grid_constant__ W
                         *reinterpret_cast<uint4*>(out + (long long)r * p.cols) = make_uint4(0, 0, 0, 0);
                 continue;
             }
-            const int buf = it & 1;
-            const uint32_t acc = tmem + buf * 256 + ((uint32_t)(quarter * 32) << 16), to = staging + (p.by_halves() ? (it & 1) * (kXStaging / 2) : 0);
-            const bool ok = mbar_wait_warp(smem_u32(&ctl->acc_full[buf]), (it >> 1) & 1, abort_flag, all.status);   // (given up: goes on without work)
+            const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16), to = staging + (p.by_halves() ? half : 0);
+            bool ok = mbar_wait_warp(smem_u32(&ctl->acc_full[it & 1]), (it >> 1) & 1, abort_flag, all.status);   // (given up: goes on without work)
             tc_fence_after();
+            // a long run: the sum so far is added to the next piece's accumulator, whose place it then has, and its own is free
+            for (int left = w.n - kRunPiece; left > 0; left -= kRunPiece) {
+                const int before = it++ & 1;
+                ok &= mbar_wait_warp(smem_u32(&ctl->acc_full[it & 1]), (it >> 1) & 1, abort_flag, all.status);
+                tc_fence_after();
+                for (int c = copy * 32; ok && c < per && row0 < rows && c0 + side * per + c < p.cols; c += copies * 32)
+                    for (int i = 0; i < 32; i += 16) {
+                        float v[16], sum[16];
+                        tmem_ld16(lanes + before * 256 + side * per + c + i, sum);
+                        tmem_ld16(lanes + (it & 1) * 256 + side * per + c + i, v);
+                        tmem_ld_wait16(sum); tmem_ld_wait16(v);
+                        uint32_t u[2][8];
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) u[j / 8][j % 8] = __float_as_uint(sum[j] + v[j]);
+                        tmem_st8(lanes + (it & 1) * 256 + side * per + c + i, u[0]);
+                        tmem_st8(lanes + (it & 1) * 256 + side * per + c + i + 8, u[1]);
+                    }
+                tmem_st_wait();
+                tc_fence_before();
+                warp_arrive(smem_u32(&ctl->acc_empty[before]), lane);
+            }
+            const int buf = it & 1;
+            const uint32_t acc = lanes + buf * 256;
             if (warp < 6) halves && p.by_halves() ? bulk_read_done<1>() : bulk_read_done<0>();
             halves = p.by_halves();
             epilogue_sync();
@@ -1032,6 +1066,7 @@ weights_kernel(const __grid_constant__ WeightsMaps m0, const __grid_constant__ W
             tc_fence_before();
             warp_arrive(smem_u32(&ctl->acc_empty[buf]), lane);
             ++it;
+            half ^= kXStaging / 2;
             fence_async_smem();
             epilogue_sync();
             // A box for each of four warps where two units' boxes fit: issuing a store takes about 200 clocks (65536 x 4 pairs of 8192
