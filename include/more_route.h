@@ -67,6 +67,7 @@ enum {
 #define MORE_M_MAX (1 << 30) /* largest M: expert ids, and the kernels' column arithmetic, are 32-bit */
 #define MORE_H_MAX 8192   /* largest h of more_experts* and more_combine* */
 #define MORE_S_MAX 8192   /* largest width s of an expert */
+#define MORE_PAIRS_MAX 0x7fff0000 /* most (token, slot) pairs T*k of more_experts* (more: MORE_ERR_TOO_LARGE) */
 
 /*
  * more_route -- route T tokens (Algorithm 1 plus the gates of Section 2 / Eq. app_softmax and the per-expert

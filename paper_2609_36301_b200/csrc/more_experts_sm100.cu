@@ -69,6 +69,7 @@ constexpr int kSumSteps = 8;
 // it is 2e-5 at most, at any length.  And what waits for an accumulator waits for a piece, well inside its budget: a run of 4e8 pairs in
 // one piece took longer than that.  One expert, h = 512, s = 64, 65536 pairs: the backward pass 1223 us with one piece, 1243 with eight.
 constexpr int kRunPiece = 8192;
+static_assert(MORE_PAIRS_MAX <= 0x7fffffff - kRunPiece, "places are counted in 32 bits");
 
 enum { kUp = 0, kDown = 1, kBackAct = 2, kBackX = 3 };
 
@@ -1351,7 +1352,7 @@ int check_sizes(int T, int h, int s, int M, int k)
 {
     if (T < 0 || h < 8 || s < 8 || h % 8 != 0 || s % 8 != 0 || h > MORE_H_MAX || s > MORE_S_MAX) return MORE_ERR_SHAPE;
     if (M < 1 || M > MORE_M_MAX || k < 1 || k > MORE_K_MAX || k > M) return MORE_ERR_SHAPE;
-    if ((long long)T * k > 0x7fffffffLL) return MORE_ERR_TOO_LARGE;            // pairs are named by int32 positions
+    if ((long long)T * k > MORE_PAIRS_MAX) return MORE_ERR_TOO_LARGE;          // places are counted in 32 bits, past a run's end by up to a piece
     return MORE_OK;
 }
 
