@@ -165,7 +165,7 @@ pairs_kernel(const __nv_bfloat16* __restrict__ X, const __nv_bfloat16* __restric
             g += gq[q];
             u += uq[q];
         }
-        act[c] = g * sigmoidf(g) * u;
+        act[c] = g * sigmoid_to_round(g) * u;
     }
     __syncthreads();
     cluster_arrive();                                  // (done with the other CTAs' parts)

@@ -608,7 +608,7 @@ rows_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUte
                     tmem_ld16(acc + cols + side * per + c, v);
                     tmem_ld_wait16(g); tmem_ld_wait16(v);
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) g[i] = g[i] * sigmoidf(g[i]) * v[i];
+                    for (int i = 0; i < 16; ++i) g[i] = g[i] * sigmoid_to_round(g[i]) * v[i];
                     st_piece(mine + c * 2, pack8(g, 0));
                     st_piece(mine + c * 2 + 16, pack8(g, 8));
                 }
