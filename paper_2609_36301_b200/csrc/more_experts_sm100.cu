@@ -955,7 +955,7 @@ weights_kernel(const __grid_constant__ WeightsMaps m0, const __grid_constant__ W
 #pragma unroll
                 for (int i = 0; i < 2; ++i) pair[i] = i * 32 + lane < left ? all.pairs[u.lo + at + i * 32 + lane] : -1;
                 issue();
-                own.which = hold(u.which);                          // (the value now; nothing that follows from the index later)
+                own.which = u.which;
                 own.first = u.lo + at;
                 own.left = left;
                 own.mt = u.mt;
