@@ -6,6 +6,8 @@ import threading
 import pytest
 import torch
 
+import layer_reference as ref
+
 pytestmark = pytest.mark.gpu
 
 binding = pytest.importorskip("paper_2609_36301_b200.binding")
@@ -49,7 +51,26 @@ def pairs_call(T, h, s, M, k, gen):
     return make
 
 
-@pytest.mark.parametrize("op", ["combine", "combine_backward", "pairs"])
+def tiles_call(T, h, s, M, k, gen):
+    """Forward and backward, each with a workspace of its own."""
+    X, W1, W2 = randn(gen, T, h).bfloat16(), (randn(gen, M, h, 2 * s) * h ** -0.5).bfloat16(), (randn(gen, M, s, h) * s ** -0.5).bfloat16()
+    idx = torch.arange(T * k, device="cuda", dtype=torch.int32).remainder(M).view(T, k)
+    offsets, pairs = ref.lists(idx, M)
+    gate, dout = randn(gen, T, k), randn(gen, T, h).bfloat16()
+
+    def make():
+        out = [torch.empty((T * k, h), device="cuda", dtype=torch.bfloat16), torch.empty((T * k, 2 * s), device="cuda", dtype=torch.bfloat16),
+               torch.empty_like(X), torch.empty_like(gate), torch.empty_like(W1), torch.empty_like(W2)]
+        ws = [torch.empty(binding.experts_workspace(T, h, s, M, k, b), device="cuda", dtype=torch.uint8) for b in (False, True)]
+
+        def call(stream):
+            binding.more_experts(X, W1, W2, idx, offsets, pairs, *out[:2], path=binding.EXPERTS_TILES, workspace=ws[0], stream=stream)
+            binding.more_experts_backward(X, W1, W2, idx, offsets, pairs, gate, out[1], dout, *out[2:], workspace=ws[1], stream=stream)
+        return out, call
+    return make
+
+
+@pytest.mark.parametrize("op", ["combine", "combine_backward", "pairs", "tiles"])
 def test_threads_with_different_sizes(op):
     gen = torch.Generator(device="cuda")
     gen.manual_seed(1)
@@ -57,6 +78,8 @@ def test_threads_with_different_sizes(op):
         kinds = [combine_call(1200, 1024, 1, gen), combine_call(1200, 2048, 4, gen)]
     elif op == "combine_backward":           # 64 and 96 KB
         kinds = [combine_backward_call(64, 1032, gen), combine_backward_call(64, 2048, gen)]
+    elif op == "tiles":
+        kinds = [tiles_call(100, 64, 24, 5, 2, gen), tiles_call(300, 264, 136, 7, 3, gen)]
     else:                                    # 8 and 33 KB
         kinds = [pairs_call(2, 64, 8, 4, 2, gen), pairs_call(2, 64, 2048, 4, 2, gen)]
     alone = []
