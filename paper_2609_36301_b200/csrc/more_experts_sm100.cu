@@ -169,6 +169,7 @@ struct Control {
     int4 rows[kTeams * kTeam][kTileRows / 4];   // of each loader's tile
 };
 static_assert(sizeof(Control) <= kXControl && kBackLoaders <= kTeams * kTeam, "control block");
+static_assert(kTeams < kSlots && kBackLoaders < kSlots && kFewLoaders < kSlots, "Ring::wait_empty");
 
 // The ring of stages, each as long as what it holds (a multiple of 1024 bytes).  Every loader, and the warp that empties it, goes
 // through the same sequence of lengths and so knows where each stage lies.
@@ -177,6 +178,7 @@ struct Ring {
     uint32_t end = 0;                     // bytes of all stages so far, gaps at the ring's end included
     int n = 0;                            // stages so far
     uint32_t begun = 0;                   // lane i < 16: `end` at which the last stage of slot i began
+    int empty = -1;                       // a loader: the last stage that it knows to be empty, and with it all before
     // Where the next stage of that length lies; `from`: the value of `end` in front of it.
     __device__ uint32_t place(uint32_t bytes, uint32_t* from)
     {
@@ -203,12 +205,30 @@ struct Ring {
         if (lane == n % kSlots) begun = from;
         return own;
     }
-    // The same, and waits until it may be written.  (*live: false if the CTA is giving up.)
+    // Waits until stage `last` is empty (see mine), for a loader that is to write `stage`.  A barrier tells a phase from the one after the
+    // next by nothing, and a wait for stage m is one for m's phase only if the stage before m in its slot is known to be empty and the
+    // one behind m cannot be.  For `last` >= stage - 16 the latter holds, as what comes behind `stage` is not emptied before it.  For the
+    // former the loader may first have to wait for stage - 16, of its own slot: of that one the stage before is known to be empty (the loader's
+    // stage before this one was at most 15 back, and it waited for one at most 16 before that) and the one behind is `stage` itself.
+    // (Needed where few long stages follow many short ones.  Without it stages in use were written over, and a launch over 62478 x 6
+    // pairs of 16083 experts, h = 432, s = 24, gave up its waits where units of dW2 follow those of dW1.)  False: the CTA is giving up.
+    __device__ bool wait_empty(int stage, int last, Control* c, volatile int* abort_flag, int* status)
+    {
+        if (last < 0) return true;
+        if (last - kSlots > empty && !wait_for(stage - kSlots, c, abort_flag, status)) return false;
+        empty = last;
+        return wait_for(last, c, abort_flag, status);
+    }
+    __device__ static bool wait_for(int stage, Control* c, volatile int* abort_flag, int* status)
+    {
+        return mbar_wait_warp(smem_u32(&c->empty[stage % kSlots]), (uint32_t)(stage / kSlots) & 1u, abort_flag, status);
+    }
+    // The same as mine, and waits until it may be written.  (*live: false if the CTA is giving up.)
     __device__ bool open(uint32_t bytes, int loader, int loaders, Control* c, int lane, volatile int* abort_flag, int* status, uint32_t* at, bool* live)
     {
         int last;
         if (!mine(bytes, loader, loaders, lane, at, &last)) return false;
-        if (last >= 0 && !mbar_wait_warp(smem_u32(&c->empty[last % kSlots]), (last / kSlots) & 1, abort_flag, status)) *live = false;
+        if (!wait_empty(n, last, c, abort_flag, status)) *live = false;
         __syncwarp();
         return *live;
     }
@@ -902,7 +922,7 @@ weights_kernel(const __grid_constant__ WeightsMaps m0, const __grid_constant__ W
         Ring rg;
         bool live = true;
         struct Own {
-            int which, first, left, mt, chunk, last, slot, pair[2];  // output, first place, rows; the stage that has to be empty, or less than 0
+            int which, first, left, mt, chunk, last, stage, pair[2]; // output, first place, rows; the stage that has to be empty, or less than 0
             uint32_t where;
         } own;
         own.left = 0;
@@ -919,12 +939,12 @@ weights_kernel(const __grid_constant__ WeightsMaps m0, const __grid_constant__ W
                 reinterpret_cast<int*>(rows)[r] = in ? all.by_k(pair) : all.T;
                 reinterpret_cast<int*>(rows)[64 + r] = in ? own.first + r : all.P;
             }
-            if (own.last >= 0 && !mbar_wait_warp(smem_u32(&ctl->empty[own.last % kSlots]), (own.last / kSlots) & 1, abort_flag, all.status)) {
+            if (!rg.wait_empty(own.stage, own.last, ctl, abort_flag, all.status)) {
                 live = false;
                 return;
             }
             __syncwarp();
-            const uint32_t full = smem_u32(&ctl->full[own.slot]);
+            const uint32_t full = smem_u32(&ctl->full[own.stage % kSlots]);
             expect_elect(full, box * (a_boxes + o.nb));
             const uint32_t a_at = ring + own.where, b_at = a_at + a_boxes * box;
             const int a_x = own.mt * 128, b_x = own.chunk * o.nb * 64;
@@ -961,7 +981,7 @@ weights_kernel(const __grid_constant__ WeightsMaps m0, const __grid_constant__ W
                 own.mt = u.mt;
                 own.chunk = u.chunk;
                 own.last = last;
-                own.slot = rg.slot();
+                own.stage = rg.n;
                 own.where = where;
                 own.pair[0] = pair[0];
                 own.pair[1] = pair[1];
