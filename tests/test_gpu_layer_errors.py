@@ -1,4 +1,6 @@
 """A launch that CUDA refuses is reported by the call that it belongs to, and by no call after it."""
+import ctypes
+
 import pytest
 import torch
 
@@ -39,17 +41,17 @@ def test_a_refused_launch_is_reported_once(op):
     other = torch.cuda.Stream()
     call(other)
     torch.cuda.synchronize()
-    graph, stream = torch.cuda.CUDAGraph(), torch.cuda.Stream()
-    with torch.cuda.stream(stream):
-        graph.capture_begin(capture_error_mode="thread_local")
-        try:
-            with pytest.raises(Exception):
-                torch.cuda.current_stream().synchronize()              # not allowed in a capture, which it makes invalid
-            with pytest.raises(binding.MoreRouteError):
-                call(stream)
-            call(other)                                                # nothing of it is left
-        finally:
-            with pytest.raises(Exception):
-                graph.capture_end()
+    runtime, stream = ctypes.CDLL("libcudart.so.12"), torch.cuda.Stream()          # (the one that torch has loaded; its graphs stay out of it)
+    handle, graph = ctypes.c_void_p(stream.cuda_stream), ctypes.c_void_p()
+    assert runtime.cudaStreamBeginCapture(handle, 1) == 0                          # (of this thread)
+    try:
+        assert runtime.cudaStreamSynchronize(handle) != 0                          # not allowed in a capture, which it makes invalid
+        with pytest.raises(binding.MoreRouteError):
+            call(stream)
+        call(other)                                                                # nothing of it is left
+    finally:
+        assert runtime.cudaStreamEndCapture(handle, ctypes.byref(graph)) != 0
+        runtime.cudaGetLastError()
     call(other)
     torch.cuda.synchronize()
+    assert float(torch.rand(8, device="cuda").sum()) > 0
