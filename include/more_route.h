@@ -273,7 +273,8 @@ int more_experts_path(int T, int h, int s, int M, int k);
  *   out_dx     device bf16 [T][h], out_dgate device fp32 [T][k], out_dw1 bf16 as W1, out_dw2 bf16 as W2; OVERWRITTEN (experts
  *              without pairs get zeros; the gate gradient of a pair whose id is outside [0, M) is 0); any of them may be NULL.
  *   workspace  as above, more_experts_workspace(T, h, s, M, k, 1) bytes.
- * The Y rows are not needed: <dout, a W2> = <dout W2^T, a>.  The order of sums is that of sorted_pairs: equal lists give equal bits.
+ * The Y rows are not needed: <dout, a W2> = <dout W2^T, a>.  The order of sums is that of sorted_pairs, in pieces of 8192 pairs of an
+ * expert: equal lists give equal bits.
  * Rounded to bf16 on the way: du and gate a, as operands of the products behind them; a slot's part of dX is kept in fp16 behind a
  * power of two per row and 32 columns.
  */

@@ -11,8 +11,9 @@
 // 16-byte load, and stays in registers between the two sums of squares, so that everything is read once and written once.  All
 // sums are 32-bit; rows are rounded where they are written.  The backward's column sums stay in registers while a CTA goes
 // through its tokens, whose rows come through a ring in shared memory; a second kernel adds the CTAs' parts in order, so that
-// results do not depend on timing.  65536 tokens of h = 2048: forward with 8 slots 2.95 GB in 430 us (6.9 TB/s), backward 1.61 GB in
-// 293 us (5.5 TB/s).
+// results do not depend on timing.  65536 tokens of h = 2048, the L2 cache overwritten in front of each call: forward with 8 slots 2.95 GB in
+// 443 to 484 us from one GPU to another (6.1 to 6.7 TB/s), backward 1.61 GB in 291 to 312 us (5.2 to 5.5 TB/s).  Figures below that compare two
+// variants are of calls one after the other, whose last writes stay in L2: the backward pass takes 290 us there.
 #include "sm100_common.cuh"
 
 namespace more {
@@ -584,7 +585,10 @@ __global__ void __launch_bounds__(1024) combine_columns_kernel(const float* part
     }
 }
 
-// How a token's row is spread: vectors of 8 columns per thread, and threads; a warp per token (and eight tokens per CTA) or a CTA.
+// How a token's row is spread: vectors of 8 columns per thread, and threads; a warp per token (and eight tokens per CTA) or a CTA.  Up to
+// eight tokens per SM, and for rows of more than 1024 columns, a CTA: 64 ... 1184 tokens of 8 slots, h = 512, 8 to 11 us against 14 to 16 with a
+// warp each, h = 1024 8 to 14 against 16.  For more tokens a warp is as good (4000: h = 256 13 us against 16 with a CTA, h = 512 20.5
+// against 19.5); in between a CTA would be up to 4 us better (1300 tokens of h = 512: 12 against 16).
 struct Spread {
     int nv, width;
     bool wide;
@@ -700,7 +704,12 @@ int more_combine(const void* Y, const float* gate, const void* residual, int res
     const bool f32 = residual_type == MORE_RESIDUAL_FP32;
 #define MORE_FORWARD(NV, WIDE) (f32 ? launch_forward<NV, WIDE, float>(p, sp.width, st) : launch_forward<NV, WIDE, __nv_bfloat16>(p, sp.width, st))
     bool done = false;
-    if (T > 148 * 8 && h >= 1024) {                                  // (two stages of the rows of 24 slots or more may not fit)
+    // Through a ring where there are more than eight tokens per SM and two stages, of 2 h k bytes and the residual's, fit its 200 KB (in bf16
+    // h = 2048: up to 24 slots, 4096: 11, 8192: 5); else a CTA per token.  us with and without it, 65536 tokens of 8 slots: h = 1024 233 and 281,
+    // 2048 440 and 524, 4096 888 and 1282; of one slot: h = 1024 147 and 145, 4104 563 and 851, 8192 676 and 1802.  Shorter rows of few slots
+    // lose with it (h = 256, one slot: 70 and 41); of many they would gain (h = 512, 8 slots: 132 and 174), as would fewer tokens of long
+    // rows (1184 of h = 4096, 8 slots: 29 and 43).
+    if (T > 148 * 8 && h >= 1024) {
         const int rc = h <= 4096 ? (f32 ? launch_ring<1, float>(p, ctx->status, st, &done) : launch_ring<1, __nv_bfloat16>(p, ctx->status, st, &done))
                                  : (f32 ? launch_ring<2, float>(p, ctx->status, st, &done) : launch_ring<2, __nv_bfloat16>(p, ctx->status, st, &done));
         if (rc != MORE_OK) return rc;

@@ -5,9 +5,10 @@
 //   c = d[token] W2[e]^T,  dgate = <c, a>,  du = gate c (silu'(u_gate) u_up, silu(u_gate)),  dX = sum over slots of du W1[e]^T
 //   dW1[e] = sum of X[token]^T du,  dW2[e] = sum of (gate a)^T d[token]
 //
-// Two kernels do all of it, both persistent with one CTA per SM: warps that load, a warp that issues the tcgen05 MMAs, eight warps
-// that read the finished accumulator (two of 256 tensor-memory columns, used in turn, so that the products of the next unit run
-// meanwhile).
+// Two kernels do all of it, both persistent with one CTA per SM: warps that load, a warp that issues the tcgen05 MMAs, and eight warps
+// behind the accumulators (two of 256 tensor-memory columns, used in turn, so that the products of the next unit run meanwhile).  All
+// eight read them where values are worked on (kUp, kBackAct) and in weights_kernel; where rows are only rounded (kDown, kBackX) four
+// read them and four write the rows out.
 //
 //   rows_kernel<MODE>   tiles of up to 128 pairs of one expert against its weights.  W1 and W2 come by TMA and are used as they are
 //                       stored, the forward products with them as MN-major operands, the backward ones as K-major ones: nothing
@@ -27,7 +28,9 @@
 // kBackAct 363 MB in 85 us, kBackX 688 MB in 115 us, the gradients of both weights 872 MB in 193 us, where issuing loads and passing
 // tiles through shared memory take as long as an SM's stores.  Few wide experts are bound by what the SMs read from L2: 32768 x 8
 // pairs of 256 experts, h = 512, s = 256, kUp 160 us, of which the MMAs alone take 82 and the gathers alone 150 (about 10 clocks per
-// row of 128 bytes), kDown 103 us.
+// row of 128 bytes), kDown 103 us.  Times of whole calls in these comments compare variants in calls one after the other, whose last
+// writes stay in L2; with that overwritten in front of each call the long ones take 4 to 12 % more (65536 x 4 pairs of 8192 experts,
+// backward: 825 us and 896 to 925).
 #include "more_experts.cuh"
 
 #include <math.h>
@@ -628,7 +631,7 @@ rows_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUte
                     tmem_ld16(acc + cols + side * per + c, v);
                     tmem_ld_wait16(g); tmem_ld_wait16(v);
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) g[i] = g[i] * sigmoid_to_round(g[i]) * v[i];
+                    for (int i = 0; i < 16; ++i) g[i] = g[i] * sigmoid_to_round(g[i]) * v[i];      // (to bf16: an operand of the second product)
                     st_piece(mine + c * 2, pack8(g, 0));
                     st_piece(mine + c * 2 + 16, pack8(g, 8));
                 }
@@ -712,6 +715,7 @@ rows_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUte
                         out_u[j] = da * silu;
                         out_g[j] = da * up * fmaf(silu, 1.f - sg, sg);
                     }
+                    // (du and gate a to bf16: operands of the products behind)
                     *reinterpret_cast<uint4*>(p.du + place * 2 * p.s + s0) = pack8(out_g);
                     *reinterpret_cast<uint4*>(p.du + place * 2 * p.s + p.s + s0) = pack8(out_u);
                     if (p.ga) *reinterpret_cast<uint4*>(p.ga + place * p.s + s0) = pack8(out_a);
@@ -1382,7 +1386,8 @@ int check_sizes(int T, int h, int s, int M, int k)
 // second, over the SMs.  Measured on eight combinations of h, s and M from 8 to 8192 pairs (us, pairs / tiles): h = 2048, s = 64,
 // M = 8192: 12 / 26 at 8 pairs, 74 / 80 at 512, 137 / 133 at 1024, 260 / 222 at 2048; h = 512, s = 64, M = 64: 14 / 20 at 128, 25 / 20
 // at 512, 38 / 20 at 1024; h = 256, s = 16, M = 16384: 46 / 46 at 2048, 136 / 103 at 8192; h = 4096, s = 512, M = 16: 68 / 46 at
-// 8.  The choice cost 2 % at worst in the run that it was fitted to, 7 % in the next.
+// 8.  The choice cost 2 % at worst in the run that it was fitted to, 7 % in the next.  (Ids that cluster hit fewer experts than evenly
+// spread ones, and tiles then take less than it says.)
 int cheaper_path(int T, int h, int s, int M, int k)
 {
     const double P = (double)T * k, weights = 6.0 * h * s, sms = 148, most = 6.2e6;     // bytes; bytes per us
